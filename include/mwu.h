@@ -353,6 +353,43 @@ int mwu_gemm_dense(int64_t rows, int64_t cols, const void *Wd, int64_t ldw, cons
                    void *cuda_stream);
 
 /*
+ * mwu_gemm_grouped, mwu_gemm_grouped_dx, mwu_gemm_grouped_dw -- products of rows sorted by group with a weight per
+ * group (Section 3.2's layer forward for a layer of experts, each of which has been compressed by itself), and their gradients.
+ * Group g holds the activation rows offsets[g] .. offsets[g + 1] - 1 and the weight W_g[rows][ldw], bf16 as
+ * mwu_decode or mwu_keep_n_of_m leave it, at Wd + g * w_stride (elements; mwu_decode pads a weight to a multiple of 128 rows).
+ *
+ *   mwu_gemm_grouped      Y[m][n]  = sum_k X[m][k] W_g[n][k]        for the rows m of every group g
+ *   mwu_gemm_grouped_dx   dX[m][k] = sum_n dY[m][n] W_g[n][k]       for the rows m of every group g
+ *   mwu_gemm_grouped_dw   dW_g[n][k] (+)= sum_{m in g} dY[m][n] X[m][k]
+ *
+ *   offsets     in   device int32 [groups + 1], in order, 0 <= offsets[0], offsets[groups] <= M; read on the device, so
+ *                    a router's output needs no trip to the host.  Offsets out of order or beyond M set MWU_DEV_BOUNDS and
+ *                    nothing is written.
+ *   X, dY       in   bf16 [M][ldx >= cols], [M][lddy >= rows]
+ *   Y, dX       out  [M][ldy >= rows], [M][lddx >= cols]; *_dtype 0: bf16, 1: fp32.  Rows of no group (before offsets[0], from
+ *                    offsets[groups] on) are left as they are, and what such rows or the rows of other groups hold in the
+ *                    inputs, NaN included, touches no result.
+ *   dW          out  dW_g [rows][lddw >= cols] at dW + g * dw_stride (elements), every group of them: a group without rows
+ *                    gets zeros.  accumulate 1 (fp32 only): added to what dW holds, groups without rows left alone.
+ * 1 <= groups <= MWU_MAX_GROUPS; rows, cols <= MWU_MAX_GROUPED_SIDE, of any value, not only multiples of something.
+ * Leading dimensions and group strides are multiples of 8 elements (fp32 outputs: of 4).  M == 0 is a no-op for the first two; the
+ * third then still writes its zeros.  Outputs must not overlap inputs.
+ * Products are bf16 x bf16 accumulated in fp32; fp32 results are summed in pieces of 512 products, so that what the
+ * tensor core drops of a long sum stays below 1e-6 of it.  The same call on the same inputs gives the same bits.
+ */
+#define MWU_MAX_GROUPS 1024
+#define MWU_MAX_GROUPED_SIDE 1048576
+int mwu_gemm_grouped(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride,
+                     const int32_t *offsets, const void *X, int64_t M, int64_t ldx, void *Y, int64_t ldy,
+                     int32_t y_dtype, uint32_t *dev_status, void *cuda_stream);
+int mwu_gemm_grouped_dx(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride,
+                        const int32_t *offsets, const void *dY, int64_t M, int64_t lddy, void *dX, int64_t lddx,
+                        int32_t dx_dtype, uint32_t *dev_status, void *cuda_stream);
+int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, const int32_t *offsets, const void *dY, int64_t M,
+                        int64_t lddy, const void *X, int64_t ldx, void *dW, int64_t lddw, int64_t dw_stride,
+                        int32_t dw_dtype, int32_t accumulate, uint32_t *dev_status, void *cuda_stream);
+
+/*
  * mwu_conv_dense -- the convolution of mwu_conv_implicit for a plain bf16 weight matrix
  * Wd[rows][ldw] whose first c*kh*kw columns are in [c][kh][kw] order (the counterpart of
  * mwu_gemm_dense; it serves the block shapes that have no packed form: project with Q, round Q to

@@ -20,7 +20,9 @@ EXPORTS = ["mwu_status_string", "mwu_kernel_launches", "mwu_count_from_permille"
            "mwu_packed_bytes", "mwu_pack", "mwu_gemm", "mwu_decode", "mwu_gemm_workspace_bytes",
            "mwu_gemm_ws", "mwu_conv_implicit", "mwu_conv_workspace_bytes", "mwu_conv_implicit_ws",
            "mwu_debug_conv_wait", "mwu_keep_n_of_m", "mwu_gemm_dense", "mwu_conv_dense_workspace_bytes",
-           "mwu_conv_dense"]
+           "mwu_conv_dense", "mwu_gemm_grouped", "mwu_gemm_grouped_dx", "mwu_gemm_grouped_dw"]
+MWU_MAX_GROUPS = 1024
+MWU_MAX_GROUPED_SIDE = 1048576
 MWU_STATIC_MAX_BLOCKS = 1048576
 
 MWU_OK = 0
@@ -103,6 +105,11 @@ def lib() -> ctypes.CDLL:
         L.mwu_conv_dense_workspace_bytes.argtypes = [i64] + [i32] * 8
         L.mwu_conv_dense.restype = ctypes.c_int
         L.mwu_conv_dense.argtypes = [i64, vp, i64, vp] + [i32] * 8 + [vp, i32, vp, sz, vp, vp]
+        for fn in (L.mwu_gemm_grouped, L.mwu_gemm_grouped_dx):
+            fn.restype = ctypes.c_int
+            fn.argtypes = [i64] * 3 + [vp, i64, i64, vp, vp, i64, i64, vp, i64, i32, vp, vp]
+        L.mwu_gemm_grouped_dw.restype = ctypes.c_int
+        L.mwu_gemm_grouped_dw.argtypes = [i64] * 3 + [vp, vp, i64, i64, vp, i64, vp, i64, i64, i32, i32, vp, vp]
         L.mwu_debug_conv_wait.restype = None
         L.mwu_debug_conv_wait.argtypes = [i64, i64]
         _lib = L
@@ -275,6 +282,35 @@ def mwu_conv_dense(rows, Wd, ldw, X, n, c, h, w, kh, kw, stride, pad, Y, y_dtype
                               _ptr(dev_status), _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_conv_dense")
+    return rc
+
+
+def mwu_gemm_grouped(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, Y, ldy, y_dtype, dev_status, stream=None,
+                     check=True) -> int:
+    rc = lib().mwu_gemm_grouped(int(groups), int(rows), int(cols), _ptr(Wd), int(ldw), int(w_stride), _ptr(offsets), _ptr(X),
+                                int(M), int(ldx), _ptr(Y), int(ldy), int(y_dtype), _ptr(dev_status), _stream(stream))
+    if check and rc != MWU_OK:
+        raise MwuError(rc, "mwu_gemm_grouped")
+    return rc
+
+
+def mwu_gemm_grouped_dx(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, lddy, dX, lddx, dx_dtype, dev_status,
+                        stream=None, check=True) -> int:
+    rc = lib().mwu_gemm_grouped_dx(int(groups), int(rows), int(cols), _ptr(Wd), int(ldw), int(w_stride), _ptr(offsets),
+                                   _ptr(dY), int(M), int(lddy), _ptr(dX), int(lddx), int(dx_dtype), _ptr(dev_status),
+                                   _stream(stream))
+    if check and rc != MWU_OK:
+        raise MwuError(rc, "mwu_gemm_grouped_dx")
+    return rc
+
+
+def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, lddw, dw_stride, dw_dtype, accumulate,
+                        dev_status, stream=None, check=True) -> int:
+    rc = lib().mwu_gemm_grouped_dw(int(groups), int(rows), int(cols), _ptr(offsets), _ptr(dY), int(M), int(lddy), _ptr(X),
+                                   int(ldx), _ptr(dW), int(lddw), int(dw_stride), int(dw_dtype), int(accumulate),
+                                   _ptr(dev_status), _stream(stream))
+    if check and rc != MWU_OK:
+        raise MwuError(rc, "mwu_gemm_grouped_dw")
     return rc
 
 

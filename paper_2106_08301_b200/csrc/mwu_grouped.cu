@@ -1,0 +1,551 @@
+// Grouped products: rows sorted by group, one weight per group, lengths that only the device knows.
+//
+//   mwu_gemm_grouped      Y[m]  = X[m] . W_g^T     reduction over cols
+//   mwu_gemm_grouped_dx   dX[m] = dY[m] . W_g      reduction over rows (of the weights)
+//   mwu_gemm_grouped_dw   dW_g  = dY_g^T . X_g     reduction over the rows of the group
+//
+// One kernel serves all three.  A cluster of two CTAs computes tiles of 256 "features" by up to 256 "lines" with
+// tcgen05.mma.cta_group::2, where features are the contiguous axis of the output and lines its rows:
+//
+//   product        features = weight rows,    lines = activation rows,  operands K-major, K-major
+//   input grad     features = weight columns, lines = gradient rows,    operands MN-major (W as it lies), K-major
+//   weight grad    features = weight columns, lines = weight rows,      operands MN-major (X), MN-major (dY)
+//
+// The weights are the M side of the instruction, so a group of few rows costs an N of 32 instead of a half empty tile of 128,
+// and a lane of tensor memory is a feature, so a warp's store of one line is one contiguous run of the output, whatever
+// the line: ragged groups need no masked box, only a test per line.
+// The groups' offsets are checked and turned into a table of tiles by every CTA at its start (device memory, no host).
+// In the weight gradient a group's last stage of 64 rows may hold rows of the next group, which must not be multiplied, not
+// even by zero (they may be NaN): such a stage is loaded onto a barrier of its own, a warp of each CTA zeroes the
+// foreign rows up to the next multiple of 16 in both operands, and only then it is handed to the issuer of the MMAs.
+// fp32 results: the tensor core drops what lies below an accumulator's last place (about 1e-9 of the result a product, always
+// towards zero), so sums are taken out of tensor memory every 512 products and added in registers; bf16 results hide it.
+//
+// Roles per CTA (11 warps): warp 0 TMA producer, warp 1 tensor memory and (leader) MMAs, warps 2 to 9 epilogue (two per
+// 32-lane quarter, every other 32 lines), warp 10 zeroes foreign rows.  Every wait on an mbarrier is bounded; when one runs
+// out the kernel raises MWU_DEV_TIMEOUT, drains what it issued, frees tensor memory and returns.
+#include "mwu_gemm_dev.cuh"
+
+namespace mwu {
+namespace gemm {
+
+EncodeTiledFn get_encode_fn();          // mwu_gemm.cu
+
+constexpr int G_STAGES = 6;
+constexpr int G_EPI_WARPS = 8;
+constexpr int G_FIX_WARP = 2 + G_EPI_WARPS;
+constexpr int G_THREADS = 32 * (3 + G_EPI_WARPS);
+constexpr int G_SIDE = 128 * 128;                    // bytes of one operand of a stage in one CTA: 128 features or lines x 64
+constexpr int G_STAGE_BYTES = 2 * G_SIDE;
+constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 64 reduction steps
+constexpr int G_LINE_BOX = 32;                       // lines of a K-major box
+constexpr int G_BAND = 8;                            // line tiles per band of the tile order
+constexpr int G_CHUNK = 8;                           // stages between two sums of an fp32 result (512 products)
+
+enum { G_FORWARD = 0, G_DX = 1, G_DW = 2 };
+
+struct GroupedParams {
+    const int *offsets;                 // [groups + 1]
+    void *out;
+    long long ldo, out_stride;          // elements between output rows, between groups (weight gradient)
+    int groups, M;
+    int features, reduction, lines;     // reduction: of a product or input gradient; lines: of a weight gradient
+    int line_tile;                      // most lines of a tile
+    int out_fp32, accumulate;
+    unsigned *dev_status;
+};
+
+struct GroupedSmem {
+    unsigned long long full[G_STAGES], empty[G_STAGES], tail[G_STAGES], peer_fixed[G_STAGES], tfull[2], tempty[2], drain;
+    unsigned tmem_base;
+    int abort, drain_abort;
+    int n_live;                         // groups with rows
+    int offsets[MWU_MAX_GROUPS + 1];
+    int cum[MWU_MAX_GROUPS + 1];        // line tiles before the i-th group with rows
+    unsigned short live[MWU_MAX_GROUPS];
+};
+
+static_assert(1024 + G_STAGES * G_STAGE_BYTES + sizeof(GroupedSmem) <= 232448, "grouped kernel: shared memory above 227 KB");
+
+__device__ __forceinline__ void tma_load_3d_pair(unsigned dst, const CUtensorMap *map, unsigned bar_cluster, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 "
+        "[%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar_cluster), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// MN-major operand, 128-byte swizzle: 64 features to a row of 128 bytes, 8 reduction steps to 1024 bytes, the next 64 features
+// G_SUB bytes on
+__device__ __forceinline__ unsigned long long make_desc_mn(unsigned smem_addr) {
+    unsigned long long d = 0;
+    d |= (unsigned long long)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (unsigned long long)(G_SUB >> 4) << 16;
+    d |= (unsigned long long)(1024 >> 4) << 32;
+    d |= (unsigned long long)1 << 46;
+    d |= (unsigned long long)2 << 61;
+    return d;
+}
+// a wait that also orders what another CTA of the cluster wrote before it arrived
+__device__ __forceinline__ bool mbar_wait_cluster(unsigned bar, unsigned parity, volatile int *abort) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (true) {
+        unsigned ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if (*abort) return false;
+        if (clock64() - t0 > WAIT_LIMIT_CYCLES) { *abort = 1; return false; }
+    }
+}
+
+struct GroupedTile {
+    int group, feature0, line0, line_count, line_pad;   // line0: row of X / dY, or weight row
+    int red0, red_len;                                  // weight gradient: first row of the group and their number
+};
+
+// Tile t.  Tiles of a group lie together; inside it they walk bands of G_BAND line tiles, feature tile by feature tile, so
+// that the pairs running at one time share a few tiles of either operand in L2.
+template <int OP>
+__device__ __forceinline__ void grouped_tile(const GroupedParams &p, const GroupedSmem *sm, unsigned t, unsigned f_tiles, GroupedTile &o) {
+    unsigned lt, n_lt, r;
+    if (OP == G_DW) {
+        n_lt = (unsigned)(p.lines + 255) / 256;
+        const unsigned per = n_lt * f_tiles, g = t / per;
+        r = t - g * per;
+        o.group = (int)g;
+        o.red0 = sm->offsets[g];
+        o.red_len = sm->offsets[g + 1] - o.red0;
+    } else {
+        const unsigned q = t / f_tiles;                     // the line tile that would be it if a group's were the outer loop
+        int lo = 0, hi = sm->n_live - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((unsigned)sm->cum[mid] <= q) lo = mid; else hi = mid - 1;
+        }
+        o.group = sm->live[lo];
+        n_lt = (unsigned)(sm->cum[lo + 1] - sm->cum[lo]);
+        r = t - (unsigned)sm->cum[lo] * f_tiles;
+    }
+    const unsigned per_band = G_BAND * f_tiles, band = r / per_band, rb = r - band * per_band;
+    const unsigned left = n_lt - band * G_BAND, wide = left < (unsigned)G_BAND ? left : (unsigned)G_BAND;
+    const unsigned ft = rb / wide;
+    lt = band * G_BAND + (rb - ft * wide);
+    o.feature0 = (int)(ft * 256);
+    if (OP == G_DW) {
+        o.line0 = (int)(lt * 256);
+        o.line_count = min(256, p.lines - o.line0);
+    } else {
+        const int begin = sm->offsets[o.group], len = sm->offsets[o.group + 1] - begin;
+        // as many lines to every tile of the group, in whole 32s: never more than line_tile, and no tile is left empty
+        const int h = (((len + (int)n_lt - 1) / (int)n_lt) + 31) & ~31;
+        o.line0 = begin + (int)lt * h;
+        o.line_count = min(h, len - (int)lt * h);
+        o.red0 = 0;
+        o.red_len = p.reduction;
+    }
+    o.line_pad = (o.line_count + 31) & ~31;
+}
+
+template <int OP>
+__global__ void __launch_bounds__(G_THREADS, 1)
+mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ CUtensorMap tmap_l,
+                        const __grid_constant__ GroupedParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *sF = smem_raw + smem_pad_1024(smem_raw);
+    unsigned char *sL = sF + G_STAGES * G_SIDE;
+    GroupedSmem *sm = reinterpret_cast<GroupedSmem *>(sL + G_STAGES * G_SIDE);
+    volatile int *abort = &sm->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned rank = cluster_rank();               // 0: leader (issues the MMAs), 1: peer
+    const unsigned pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const unsigned f_tiles = (unsigned)(p.features + 255) / 256;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < G_STAGES; ++s) {
+            mbar_init(smem_u32(&sm->full[s]), 1);
+            mbar_init(smem_u32(&sm->empty[s]), 1);
+            mbar_init(smem_u32(&sm->tail[s]), 1);
+            mbar_init(smem_u32(&sm->peer_fixed[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&sm->tfull[b]), 1);
+            mbar_init(smem_u32(&sm->tempty[b]), 2 * G_EPI_WARPS);
+        }
+        mbar_init(smem_u32(&sm->drain), 1);
+        sm->abort = 0;
+        sm->drain_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc2(smem_u32(&sm->tmem_base), 512);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // the groups: offsets in order and inside the rows that there are, or nothing is done at all
+    int bad = 0;
+    for (int i = threadIdx.x; i <= p.groups; i += G_THREADS) {
+        const int v = __ldg(p.offsets + i), before = i ? __ldg(p.offsets + i - 1) : 0;
+        sm->offsets[i] = v;
+        bad |= v < before || v > p.M;
+    }
+    bad = __syncthreads_or(bad);
+    if (bad && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_BOUNDS);
+    if (OP != G_DW && warp == 2) {
+        int n = 0, tiles = 0;
+        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            const int len = g < p.groups && !bad ? sm->offsets[g + 1] - sm->offsets[g] : 0;
+            const int mine = len > 0 ? (int)(((unsigned)len + (unsigned)p.line_tile - 1) / (unsigned)p.line_tile) : 0;
+            int upto = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int o = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += o;
+            }
+            const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
+            if (mine) {
+                const int at = n + __popc(some & ((1u << lane) - 1u));
+                sm->live[at] = (unsigned short)g;
+                sm->cum[at] = tiles + upto - mine;
+            }
+            n += __popc(some);
+            tiles += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        if (lane == 0) {
+            sm->cum[n] = tiles;
+            sm->n_live = n;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                 // both CTAs' barriers exist before any remote arrive
+    tc_fence_after();
+    const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
+    // (the host refuses sizes whose tile count could pass 2^31)
+    const unsigned total = bad ? 0u : OP == G_DW ? (unsigned)p.groups * f_tiles * ((unsigned)(p.lines + 255) / 256)
+                                                 : (unsigned)sm->cum[sm->n_live] * f_tiles;
+    GroupedTile t;
+
+    if (warp == 0) {
+        // ---------------- TMA producer: this CTA's halves of both operands ----------------
+        int stage = 0;
+        unsigned phase = 0, tails = 0;                     // tails: bit s set after an odd number of them in slot s
+        bool ok = true;
+        for (unsigned k = pair; ok && k < total; k += n_pairs) {
+            grouped_tile<OP>(p, sm, k, f_tiles, t);
+            const int n_st = (t.red_len + 63) / 64, half = t.line_pad / 2;
+            const int f0 = t.feature0 + (int)rank * 128, l0 = t.line0 + (int)rank * half;
+            const int boxes = OP == G_DW ? (half + 63) / 64 : (half + G_LINE_BOX - 1) / G_LINE_BOX;
+            const unsigned bytes = (unsigned)G_SIDE + (unsigned)boxes * (OP == G_DW ? G_SUB : G_LINE_BOX * 128);
+            for (int ks = 0; ks < n_st; ++ks) {
+                if (!mbar_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort)) ok = false;
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                const bool tail = OP == G_DW && t.red_len - ks * 64 < 64 && ((t.red_len - ks * 64) & 15);
+                if (elect_one()) {
+                    const unsigned df = smem_u32(sF + stage * G_SIDE), dl = smem_u32(sL + stage * G_SIDE);
+                    const int r0 = ks * 64;
+                    if (tail) {
+                        // foreign rows to zero: onto this CTA's own barrier, the fixing warp hands the stage on.  (A barrier to a
+                        // slot: the next group's last stage may be under way before this one has landed.)
+                        const unsigned bar = smem_u32(&sm->tail[stage]);
+                        mbar_expect_tx(bar, bytes);
+                        tma_load_2d(df, &tmap_f, bar, f0, t.red0 + r0);
+                        tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
+                        for (int b = 0; b < boxes; ++b) tma_load_2d(dl + b * G_SUB, &tmap_l, bar, l0 + 64 * b, t.red0 + r0);
+                    } else {
+                        const unsigned bar = mbar_addr_in_cta(smem_u32(&sm->full[stage]), 0);
+                        if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), 2 * bytes);
+                        if (OP == G_FORWARD) {
+                            tma_load_3d_pair(df, &tmap_f, bar, r0, f0, t.group);
+                        } else if (OP == G_DX) {
+                            tma_load_3d_pair(df, &tmap_f, bar, f0, r0, t.group);
+                            tma_load_3d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, r0, t.group);
+                        } else {
+                            tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
+                            tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
+                        }
+                        for (int b = 0; b < boxes; ++b) {
+                            if (OP == G_DW) tma_load_2d_pair(dl + b * G_SUB, &tmap_l, bar, l0 + 64 * b, t.red0 + r0);
+                            else tma_load_2d_pair(dl + b * G_LINE_BOX * 128, &tmap_l, bar, r0, l0 + G_LINE_BOX * b);
+                        }
+                    }
+                }
+                __syncwarp();
+                tails ^= (unsigned)tail << stage;
+                if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+        // a wait ran out: the loads in flight (of both CTAs, as far as they were issued) land before anybody leaves
+        if (__any_sync(0xffffffffu, *abort)) {
+            volatile int *drain_abort = &sm->drain_abort;
+            if (rank == 0)
+                for (int s = 0; s < G_STAGES; ++s) mbar_wait(smem_u32(&sm->full[s]), s < stage ? phase : phase ^ 1u, drain_abort);
+            for (int s = 0; s < G_STAGES; ++s) mbar_wait(smem_u32(&sm->tail[s]), ((tails >> s) & 1u) ^ 1u, drain_abort);
+            __syncwarp();
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ---------------- MMA issuer (leader) ----------------
+        int stage = 0;
+        unsigned phase = 0, use = 0;
+        bool ok = true;
+        for (unsigned k = pair; ok && k < total; k += n_pairs) {
+            grouped_tile<OP>(p, sm, k, f_tiles, t);
+            const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
+            const unsigned idesc = make_idesc_pair(t.line_pad) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
+            for (int c0 = 0; ok && c0 < n_st; c0 += chunk, ++use) {
+                const unsigned buf = use & 1u;
+                if (!mbar_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort)) ok = false;
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_fence_after();
+                const int c1 = min(n_st, c0 + chunk);
+                for (int ks = c0; ks < c1; ++ks) {
+                    if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned af = smem_u32(sF + stage * G_SIDE), al = smem_u32(sL + stage * G_SIDE);
+                    const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
+                    const unsigned long long ldesc = OP == G_DW ? make_desc_mn(al) : make_desc(al);
+                    const int steps = min(4, (t.red_len - ks * 64 + 15) / 16);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            if (k4 < steps)                 // 16 products on: 32 bytes K-major, two groups of 8 rows MN-major
+                                umma2_bf16(tmem_base + buf * 256u, fdesc + (unsigned long long)(k4 * (OP == G_FORWARD ? 2 : 128)),
+                                           ldesc + (unsigned long long)(k4 * (OP == G_DW ? 128 : 2)), idesc, (ks > c0 || k4) ? 1u : 0u);
+                        umma2_commit_both(smem_u32(&sm->empty[stage]));
+                    }
+                    if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                if (elect_one()) umma2_commit_both(smem_u32(&sm->tfull[buf]));
+                __syncwarp();
+            }
+        }
+        // everything this thread issued must have retired before tensor memory is freed
+        if (elect_one()) umma2_commit_local(smem_u32(&sm->drain));
+        __syncwarp();
+        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort);
+        __syncwarp();
+    } else if (warp == G_FIX_WARP) {
+        // ---------------- foreign rows of a group's last stage ----------------
+        if (OP == G_DW) {
+            unsigned pos = 0, tails = 0;                    // pos: place of the tile's first stage in the ring; tails as in the producer
+            bool ok = true;
+            for (unsigned k = pair; ok && k < total; k += n_pairs) {
+                grouped_tile<OP>(p, sm, k, f_tiles, t);
+                const unsigned n_st = (unsigned)(t.red_len + 63) / 64;
+                const int rem = t.red_len & 63;
+                if (rem & 15) {
+                    const unsigned stage = (pos + n_st - 1) % G_STAGES;
+                    ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort);
+                    if (!ok) break;
+                    // rows rem .. of the next multiple of 16, 128 bytes each, in the sub-tiles of either operand
+                    const int rows = 16 - (rem & 15);
+                    for (int i = lane; i < rows * 32; i += 32) {
+                        const int r = rem + (i >> 5), sub = (i >> 3) & 3, piece = i & 7;
+                        unsigned char *side = sub < 2 ? sF : sL;
+                        *reinterpret_cast<uint4 *>(side + stage * G_SIDE + (sub & 1) * G_SUB + r * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (rank) {
+                        if (lane == 0) mbar_arrive_cluster(smem_u32(&sm->peer_fixed[stage]), 0);
+                    } else {
+                        ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&sm->peer_fixed[stage]), (tails >> stage) & 1u, abort));
+                        if (!ok) break;
+                        fence_proxy_async();
+                        if (lane == 0) mbar_arrive(smem_u32(&sm->full[stage]));
+                    }
+                    __syncwarp();
+                    tails ^= 1u << stage;
+                }
+                pos = (pos + n_st) % G_STAGES;
+            }
+        }
+    } else if (warp >= 2) {
+        // ---------------- epilogue: this CTA's 128 features x the tile's lines ----------------
+        const int quarter = warp & 3;                       // TMEM lanes this warp may read
+        const int odd = (warp - 2) >> 2;                    // its share: every other 32 lines
+        unsigned use = 0;
+        bool ok = true;
+        for (unsigned k = pair; ok && k < total; k += n_pairs) {
+            grouped_tile<OP>(p, sm, k, f_tiles, t);
+            const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
+            float acc[4][32];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) acc[q][j] = 0.f;
+            for (int c0 = 0; c0 < n_st; c0 += chunk, ++use) {
+                const unsigned buf = use & 1u;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull[buf]), (use >> 1) & 1u, abort));
+                if (!ok) break;
+                tc_fence_after();
+                const unsigned trow = tmem_base + ((unsigned)(quarter * 32) << 16) + buf * 256u + (unsigned)(odd * 32);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (64 * q + 32 * odd < t.line_pad) {
+                        unsigned v[32];
+                        tmem_ld32(trow + (unsigned)(64 * q), v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[q][j] += __uint_as_float(v[j]);
+                    }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (rank == 0) mbar_arrive(smem_u32(&sm->tempty[buf]));
+                    else mbar_arrive_cluster(smem_u32(&sm->tempty[buf]), 0);
+                }
+            }
+            if (!ok) break;
+            const int f = t.feature0 + (int)rank * 128 + quarter * 32 + lane;
+            // (accumulating: a group without rows adds nothing)
+            const int lines = f >= p.features || (OP == G_DW && p.accumulate && n_st == 0) ? 0 : t.line_count;
+            const long long row0 = (OP == G_DW ? t.group * p.out_stride : 0ll) + (long long)t.line0 * p.ldo + f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int l0 = 64 * q + 32 * odd;
+                if (l0 >= lines) break;
+                const int n = min(32, lines - l0);
+                if (p.out_fp32) {
+                    float *dst = reinterpret_cast<float *>(p.out) + row0 + l0 * p.ldo;
+                    if (OP == G_DW && p.accumulate) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < n) acc[q][j] += dst[j * p.ldo];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < n) dst[j * p.ldo] = acc[q][j];
+                } else {
+                    __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + row0 + l0 * p.ldo;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < n) dst[j * p.ldo] = __float2bfloat16_rn(acc[q][j]);
+                }
+            }
+            __syncwarp();
+        }
+    }
+
+    // teardown: nobody leaves while the other CTA may still read this one's memory or barriers
+    tc_fence_before();
+    __syncthreads();
+    if (*abort && threadIdx.x == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_TIMEOUT);
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc2(tmem_base, 512);
+    }
+}
+
+template <int OP>
+static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const CUtensorMap &tmap_l, const GroupedParams &p, long long most_tiles,
+                                  int sm_count, cudaStream_t st) {
+    auto kern = mwu_gemm_grouped_kernel<OP>;
+    const size_t smem = 1024 + (size_t)G_STAGES * G_STAGE_BYTES + sizeof(GroupedSmem);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const long long pairs = most_tiles < sm_count / 2 ? most_tiles : sm_count / 2;
+    count_launch();
+    return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, tmap_l, p);
+}
+
+// box of 64 elements of the contiguous axis by `box_rows`, one group
+static bool encode_bf16(EncodeTiledFn encode, CUtensorMap *tm, const void *ptr, int64_t inner, int64_t rows, int64_t ld, int box_rows,
+                        int64_t groups, int64_t stride) {
+    const cuuint64_t gdim[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)groups};
+    const cuuint64_t gstride[2] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)BK, (cuuint32_t)box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups ? 3 : 2, const_cast<void *>(ptr), gdim, gstride, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Y = X . W^T and dX = dY . W: `red` / `features` = cols / rows of the weights, or rows / cols
+template <int OP>
+static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride, const int32_t *offsets,
+                     const void *in, int64_t M, int64_t ldi, void *out, int64_t ldo, int32_t out_dtype, uint32_t *dev_status,
+                     void *cuda_stream) {
+    const int64_t features = OP == G_FORWARD ? rows : cols, red = OP == G_FORWARD ? cols : rows;
+    if (!Wd || !offsets || !in || !out || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if (out_dtype != 0 && out_dtype != 1) return MWU_ERR_INVALID_ARG;
+    if (groups <= 0 || groups > MWU_MAX_GROUPS || rows <= 0 || cols <= 0 || ldw < cols || ldi < red || ldo < features) return MWU_ERR_SHAPE;
+    if (rows > MWU_MAX_GROUPED_SIDE || cols > MWU_MAX_GROUPED_SIDE || M >= (int64_t(1) << 31) - 256) return MWU_ERR_SHAPE;
+    if (ldw >= (int64_t(1) << 31) || ldi >= (int64_t(1) << 31) || ldo >= (int64_t(1) << 31)) return MWU_ERR_SHAPE;
+    if (w_stride < rows * ldw || w_stride >= (int64_t(1) << 38)) return MWU_ERR_SHAPE;
+    if (!aligned_to(Wd, 16) || !aligned_to(in, 16) || !aligned_to(out, 16) || !aligned_to(offsets, 4) || !aligned_to(dev_status, 4) ||
+        ldw % 8 != 0 || w_stride % 8 != 0 || ldi % 8 != 0 || ldo % (out_dtype ? 4 : 8) != 0)
+        return MWU_ERR_ALIGNMENT;
+    GroupedParams p = {};
+    p.offsets = offsets;
+    p.out = out; p.ldo = ldo; p.out_fp32 = out_dtype;
+    p.groups = (int)groups; p.M = (int)M; p.features = (int)features; p.reduction = (int)red;
+    p.line_tile = 256;
+    p.dev_status = dev_status;
+    const int64_t f_tiles = (features + 255) / 256;
+    const int64_t most = (M / p.line_tile + (M < groups ? M : groups)) * f_tiles;
+    if (most >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
+    int sm_count = 0;
+    const int rc = check_device(&sm_count);
+    if (rc != MWU_OK) return rc;
+    if (M == 0) return MWU_OK;
+    EncodeTiledFn encode = get_encode_fn();
+    if (!encode) return MWU_ERR_CUDA;
+    CUtensorMap tmap_f, tmap_l;
+    if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? 128 : 64, groups, w_stride) ||
+        !encode_bf16(encode, &tmap_l, in, red, M, ldi, G_LINE_BOX, 0, 0))
+        return MWU_ERR_CUDA;
+    return launch_grouped<OP>(tmap_f, tmap_l, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+}
+
+}  // namespace gemm
+}  // namespace mwu
+
+extern "C" int mwu_gemm_grouped(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride,
+                                const int32_t *offsets, const void *X, int64_t M, int64_t ldx, void *Y, int64_t ldy, int32_t y_dtype,
+                                uint32_t *dev_status, void *cuda_stream) {
+    using namespace mwu::gemm;
+    return run_lines<G_FORWARD>(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, Y, ldy, y_dtype, dev_status, cuda_stream);
+}
+
+extern "C" int mwu_gemm_grouped_dx(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride,
+                                   const int32_t *offsets, const void *dY, int64_t M, int64_t lddy, void *dX, int64_t lddx,
+                                   int32_t dx_dtype, uint32_t *dev_status, void *cuda_stream) {
+    using namespace mwu::gemm;
+    return run_lines<G_DX>(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, lddy, dX, lddx, dx_dtype, dev_status, cuda_stream);
+}
+
+extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, const int32_t *offsets, const void *dY, int64_t M,
+                                   int64_t lddy, const void *X, int64_t ldx, void *dW, int64_t lddw, int64_t dw_stride,
+                                   int32_t dw_dtype, int32_t accumulate, uint32_t *dev_status, void *cuda_stream) {
+    using namespace mwu;
+    using namespace mwu::gemm;
+    if (!offsets || !dY || !X || !dW || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if ((dw_dtype != 0 && dw_dtype != 1) || (accumulate != 0 && accumulate != 1) || (accumulate && !dw_dtype)) return MWU_ERR_INVALID_ARG;
+    if (groups <= 0 || groups > MWU_MAX_GROUPS || rows <= 0 || cols <= 0 || lddy < rows || ldx < cols || lddw < cols) return MWU_ERR_SHAPE;
+    if (rows > MWU_MAX_GROUPED_SIDE || cols > MWU_MAX_GROUPED_SIDE || M >= (int64_t(1) << 31) - 256) return MWU_ERR_SHAPE;
+    if (lddy >= (int64_t(1) << 31) || ldx >= (int64_t(1) << 31) || lddw >= (int64_t(1) << 31)) return MWU_ERR_SHAPE;
+    if (dw_stride < rows * lddw || dw_stride >= (int64_t(1) << 38)) return MWU_ERR_SHAPE;
+    if (!aligned_to(dY, 16) || !aligned_to(X, 16) || !aligned_to(dW, 16) || !aligned_to(offsets, 4) || !aligned_to(dev_status, 4) ||
+        lddy % 8 != 0 || ldx % 8 != 0 || lddw % (dw_dtype ? 4 : 8) != 0 || dw_stride % (dw_dtype ? 4 : 8) != 0)
+        return MWU_ERR_ALIGNMENT;
+    GroupedParams p = {};
+    p.offsets = offsets;
+    p.out = dW; p.ldo = lddw; p.out_stride = dw_stride; p.out_fp32 = dw_dtype; p.accumulate = accumulate;
+    p.groups = (int)groups; p.M = (int)M; p.features = (int)cols; p.lines = (int)rows;
+    p.line_tile = 256;
+    p.dev_status = dev_status;
+    const int64_t tiles = groups * ((rows + 255) / 256) * ((cols + 255) / 256);
+    if (tiles >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
+    int sm_count = 0;
+    const int rc = check_device(&sm_count);
+    if (rc != MWU_OK) return rc;
+    EncodeTiledFn encode = get_encode_fn();
+    if (!encode) return MWU_ERR_CUDA;
+    CUtensorMap tmap_f, tmap_l;
+    const int64_t m_rows = M > 0 ? M : 1;               // no rows: the maps are never used, the gradients are zeros
+    if (!encode_bf16(encode, &tmap_f, X, cols, m_rows, ldx, 64, 0, 0) || !encode_bf16(encode, &tmap_l, dY, rows, m_rows, lddy, 64, 0, 0))
+        return MWU_ERR_CUDA;
+    return launch_grouped<G_DW>(tmap_f, tmap_l, p, tiles, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+}
