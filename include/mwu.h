@@ -390,6 +390,39 @@ int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, const int32_
                         int32_t dw_dtype, int32_t accumulate, uint32_t *dev_status, void *cuda_stream);
 
 /*
+ * mwu_adapters_add -- low-rank adapters of many requests beside a shared projection (not in the paper: what a task needs beyond
+ * a compressed layer that all requests share, added to that layer's output):
+ *
+ *   Y[m][n] = Y0[m][n] + scale[a] * sum_j (sum_k X[m][k] A_a[j][k]) B_a[n][j]      for the rows m of a segment with adapter a
+ *
+ * A batch is cut into segments (one request each): segment s holds rows offsets[s] .. offsets[s + 1] - 1 and has adapter
+ * which[s]; -1 is none, Y = Y0.  Segments may be empty, of one row (generation) or of thousands (prompts), share adapters, and
+ * come in any order of adapters.
+ *
+ *   A, B         in   bf16; A_a [rank][lda >= cols] at A + a * a_stride, B_a [rows][ldb >= rank] at B + a * b_stride (elements)
+ *   scale        in   device fp32 [adapters], or NULL: 1
+ *   offsets      in   device int32 [segments + 1], in order, 0 <= offsets[0], offsets[segments] <= M
+ *   which        in   device int32 [segments], -1 .. adapters - 1.  Both are read on the device; lists that break these rules
+ *                     set MWU_DEV_BOUNDS and nothing is written.
+ *   X            in   bf16 [M][ldx >= cols], the input of the shared projection
+ *   Y0           in   its output, [M][ldy >= rows], of Y's type; may be Y itself (added in place) or NULL (zeros), and must not
+ *                     overlap Y otherwise
+ *   Y            out  [M][ldy]; y_dtype 0: bf16, 1: fp32.  Rows of no segment are left as they are.
+ * 1 <= rank <= MWU_MAX_RANK, segments <= MWU_MAX_SEGMENTS, rows and cols <= MWU_MAX_GROUPED_SIDE, of any value; lda, ldb, ldx, a_stride,
+ * b_stride and a bf16 ldy are multiples of 8 elements, an fp32 ldy of 4.  X A^T is held in fp32 and enters the second product as
+ * bf16 terms (two for a bf16 Y, three for fp32), so no rounding but Y's own shows.  The same call on the same
+ * inputs gives the same bits.  For training, the gradients are grouped products with a side as long as the rank, of the rows sorted
+ * by adapter: T = X A^T (mwu_gemm_grouped), dT = dY B and dX = dT A (mwu_gemm_grouped_dx), dA = dT^T X and dB = dY^T T
+ * (mwu_gemm_grouped_dw), the scale folded into B.
+ */
+#define MWU_MAX_RANK 128
+#define MWU_MAX_SEGMENTS 4096
+int mwu_adapters_add(int64_t adapters, int64_t rank, int64_t rows, int64_t cols, const void *A, int64_t lda, int64_t a_stride,
+                     const void *B, int64_t ldb, int64_t b_stride, const float *scale, int64_t segments,
+                     const int32_t *offsets, const int32_t *which, const void *X, int64_t M, int64_t ldx, const void *Y0,
+                     void *Y, int64_t ldy, int32_t y_dtype, uint32_t *dev_status, void *cuda_stream);
+
+/*
  * mwu_conv_dense -- the convolution of mwu_conv_implicit for a plain bf16 weight matrix
  * Wd[rows][ldw] whose first c*kh*kw columns are in [c][kh][kw] order (the counterpart of
  * mwu_gemm_dense; it serves the block shapes that have no packed form: project with Q, round Q to

@@ -20,9 +20,12 @@ EXPORTS = ["mwu_status_string", "mwu_kernel_launches", "mwu_count_from_permille"
            "mwu_packed_bytes", "mwu_pack", "mwu_gemm", "mwu_decode", "mwu_gemm_workspace_bytes",
            "mwu_gemm_ws", "mwu_conv_implicit", "mwu_conv_workspace_bytes", "mwu_conv_implicit_ws",
            "mwu_debug_conv_wait", "mwu_keep_n_of_m", "mwu_gemm_dense", "mwu_conv_dense_workspace_bytes",
-           "mwu_conv_dense", "mwu_gemm_grouped", "mwu_gemm_grouped_dx", "mwu_gemm_grouped_dw"]
+           "mwu_conv_dense", "mwu_gemm_grouped", "mwu_gemm_grouped_dx", "mwu_gemm_grouped_dw",
+           "mwu_adapters_add"]
 MWU_MAX_GROUPS = 1024
 MWU_MAX_GROUPED_SIDE = 1048576
+MWU_MAX_RANK = 128
+MWU_MAX_SEGMENTS = 4096
 MWU_STATIC_MAX_BLOCKS = 1048576
 
 MWU_OK = 0
@@ -110,6 +113,8 @@ def lib() -> ctypes.CDLL:
             fn.argtypes = [i64] * 3 + [vp, i64, i64, vp, vp, i64, i64, vp, i64, i32, vp, vp]
         L.mwu_gemm_grouped_dw.restype = ctypes.c_int
         L.mwu_gemm_grouped_dw.argtypes = [i64] * 3 + [vp, vp, i64, i64, vp, i64, vp, i64, i64, i32, i32, vp, vp]
+        L.mwu_adapters_add.restype = ctypes.c_int
+        L.mwu_adapters_add.argtypes = ([i64] * 4 + [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, vp, vp, i64, i32, vp, vp])
         L.mwu_debug_conv_wait.restype = None
         L.mwu_debug_conv_wait.argtypes = [i64, i64]
         _lib = L
@@ -311,6 +316,16 @@ def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, ld
                                    _ptr(dev_status), _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped_dw")
+    return rc
+
+
+def mwu_adapters_add(adapters, rank, rows, cols, A, lda, a_stride, Bm, ldb, b_stride, scale, segments, offsets, which, X, M,
+                     ldx, Y0, Y, ldy, y_dtype, dev_status, stream=None, check=True) -> int:
+    rc = lib().mwu_adapters_add(int(adapters), int(rank), int(rows), int(cols), _ptr(A), int(lda), int(a_stride), _ptr(Bm),
+                                int(ldb), int(b_stride), _ptr(scale), int(segments), _ptr(offsets), _ptr(which), _ptr(X), int(M),
+                                int(ldx), _ptr(Y0), _ptr(Y), int(ldy), int(y_dtype), _ptr(dev_status), _stream(stream))
+    if check and rc != MWU_OK:
+        raise MwuError(rc, "mwu_adapters_add")
     return rc
 
 

@@ -1,0 +1,829 @@
+// mwu_adapters_add: low-rank adapters of many requests beside a shared projection,
+//
+//   Y[m] = Y0[m] + s_a (X[m] . A_a^T) . B_a^T        a = the adapter of the segment that row m lies in
+//
+// with A_a [rank][cols], B_a [rows][rank], segments (requests) of any length.  Everything about it is bytes: the adapters
+// are read once, X and Y0 in, Y out, 2 * rank products to a byte or less.  Both products run in one kernel, so T = X . A^T never
+// goes to memory.  CTAs of a cluster share the reduction of the first product (a slice of cols each), add up T through
+// distributed shared memory, and share the columns of the second (a slice of rows of B each); T is held in fp32 and enters the
+// second product as two bf16 terms, three where Y is fp32 (2^-18, 2^-27 of it), so that only Y's own rounding shows.
+//
+// Segments of up to FEW_ROWS rows (generation) and longer ones (prompts) take different kernels, both decide on the
+// device which segments are theirs, and where both are launched they run at the same time:
+//   mwu_adapters_few_kernel   16 rows to a cluster of 8 CTAs, mma.sync straight from global memory (the operands are read once and
+//                             the tensor work is nothing; a lane's eight consecutive elements stand for a permuted reduction order)
+//   mwu_adapters_tile_kernel  128 rows to a cluster of 1 to 8 CTAs, TMA and tcgen05.mma, Y0 and Y through shared memory
+//
+// Every wait on an mbarrier is bounded; when one runs out the kernel raises MWU_DEV_TIMEOUT, waits for its copies in
+// flight, frees tensor memory and returns.
+#include "mwu_gemm_dev.cuh"
+
+namespace mwu {
+namespace gemm {
+EncodeTiledFn get_encode_fn();          // mwu_gemm.cu
+}  // namespace gemm
+
+namespace adapters {
+using namespace gemm;
+
+constexpr int FEW_ROWS = 32;            // rows of a segment that the first kernel takes
+constexpr int FEW_CTAS = 8;
+constexpr int FEW_THREADS = 256;
+constexpr int TILE_THREADS = 320;
+
+struct Params {
+    const __nv_bfloat16 *A, *B, *X;
+    long long lda, a_stride, ldb, b_stride, ldx, ldy;
+    const float *scale;
+    const int *offsets, *which;
+    const void *Y0;
+    void *Y;
+    int adapters, rank, rows, cols, segments, M;
+    int beside;                         // the few-rows kernel runs beside the tile kernel launched before it
+    unsigned *dev_status;
+};
+
+// ------------------------------------------------------------------------------------------
+// which rows a cluster works on
+// ------------------------------------------------------------------------------------------
+struct Finder {
+    int warp_sum[32];
+    int item, row0, count, adapter;
+};
+
+// rows of a segment that lie in one work item, or 0 where the segment is the other kernel's
+template <bool FEW>
+__device__ __forceinline__ int item_rows(int len) { return (len <= FEW_ROWS) == FEW ? (FEW ? 16 : 128) : 0; }
+
+// Thread i looks after segments i * per .. of the list; its items are number `first` and on.  Returns how many there are in all,
+// -1 where the list makes no sense.  All threads of the CTA.
+template <bool FEW, int THREADS>
+__device__ __forceinline__ int count_items(const Params &p, Finder *f, int per, int &first) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, s0 = threadIdx.x * per;
+    int bad = 0, mine = 0;
+    for (int s = s0; s < s0 + per && s < p.segments; ++s) {
+        const int a = __ldg(p.offsets + s), b = __ldg(p.offsets + s + 1), w = __ldg(p.which + s);
+        const bool wrong = a < 0 || b < a || b > p.M || w < -1 || w >= p.adapters;
+        bad |= wrong;
+        const int unit = wrong ? 0 : item_rows<FEW>(b - a);
+        if (unit) mine += (b - a + unit - 1) / unit;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) f->warp_sum[warp] = upto;
+    bad = __syncthreads_or(bad);
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const int v = f->warp_sum[w];
+        if (w < warp) before += v;
+        total += v;
+    }
+    first = before + upto - mine;
+    return bad ? -1 : total;
+}
+
+// the thread that looks after item `item` says where it is; the others read it behind the barrier that follows
+template <bool FEW>
+__device__ __forceinline__ void find_item(const Params &p, Finder *f, int per, int first, int item) {
+    if (item < first) return;
+    int at = first;
+    for (int s = threadIdx.x * per; s < (int)(threadIdx.x + 1) * per && s < p.segments; ++s) {
+        const int a = __ldg(p.offsets + s), len = __ldg(p.offsets + s + 1) - a, unit = item_rows<FEW>(len);
+        const int n = unit ? (len + unit - 1) / unit : 0;
+        if (item < at + n) {
+            const int r = (item - at) * unit;
+            f->row0 = a + r;
+            f->count = min(unit, len - r);
+            f->adapter = __ldg(p.which + s);
+            return;
+        }
+        at += n;
+    }
+}
+
+// Y = Y0 (or zeros) for rows without an adapter, columns n0 .. n1 (n0 a multiple of 32), 16 bytes at a time
+template <bool F32>
+__device__ __forceinline__ void copy_rows(const Params &p, int row0, int count, int n0, int n1, int tid, int threads) {
+    if (p.Y0 == p.Y || n1 <= n0) return;
+    constexpr int SIZE = F32 ? 4 : 2, UNIT = 16 / SIZE;
+    const unsigned char *from = reinterpret_cast<const unsigned char *>(p.Y0);
+    unsigned char *to = reinterpret_cast<unsigned char *>(p.Y);
+    const unsigned units = (unsigned)(n1 - n0 + UNIT - 1) / UNIT;
+    for (unsigned e = tid; e < units * (unsigned)count; e += threads) {
+        const unsigned r = e / units;
+        const int n = n0 + (int)(e - r * units) * UNIT;
+        const long long at = ((long long)(row0 + (int)r) * p.ldy + n) * SIZE;
+        if (n + UNIT <= n1) {
+            *reinterpret_cast<uint4 *>(to + at) = from ? *reinterpret_cast<const uint4 *>(from + at) : make_uint4(0, 0, 0, 0);
+        } else {
+            for (int b = 0; b < (n1 - n) * SIZE; b += 2)
+                *reinterpret_cast<unsigned short *>(to + at + b) = from ? *reinterpret_cast<const unsigned short *>(from + at + b) : (unsigned short)0;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// few rows
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the first `valid` of a word's two halves of elements e, e + 1
+__device__ __forceinline__ unsigned keep_valid(unsigned w, int e, int valid) {
+    return e + 1 < valid ? w : (e < valid ? w & 0xffffu : 0u);
+}
+// eight consecutive elements of a row that has `valid` left from here
+__device__ __forceinline__ uint4 load8(const __nv_bfloat16 *at, int valid) {
+    if (valid <= 0) return make_uint4(0, 0, 0, 0);
+    uint4 v = __ldg(reinterpret_cast<const uint4 *>(at));
+    if (valid < 8) {
+        v.x = keep_valid(v.x, 0, valid);
+        v.y = keep_valid(v.y, 2, valid);
+        v.z = keep_valid(v.z, 4, valid);
+        v.w = keep_valid(v.w, 6, valid);
+    }
+    return v;
+}
+__device__ __forceinline__ uint2 load4(const __nv_bfloat16 *at, int valid) {
+    if (valid <= 0) return make_uint2(0, 0);
+    uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
+    if (valid < 4) {
+        v.x = keep_valid(v.x, 0, valid);
+        v.y = keep_valid(v.y, 2, valid);
+    }
+    return v;
+}
+__device__ __forceinline__ float remote_f32(unsigned local, unsigned cta) {
+    unsigned at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(cta));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+template <int R, bool F32>
+struct Few {
+    static constexpr int TERMS = F32 ? 3 : 2;
+    static constexpr int T_LD = R + 8;                      // elements of a row of T: the eight rows of a load fall into different banks
+    float red[FEW_THREADS / 32][16][R];
+    float part[16][R];
+    __nv_bfloat16 T[TERMS][16][T_LD];
+};
+
+// 16 rows of one segment to a cluster.  First product: CTA c of the cluster takes an eighth of cols in chunks of 32, a warp a
+// chunk at a time: lane (g, t) = (lane / 4, lane % 4) loads elements 8t .. 8t + 7 of the chunk of rows g and g + 8 of X and of rows
+// 8i + g of A, 16 bytes each, and the two MMAs of a chunk take words 0, 1 and 2, 3 of both: the order of the reduction is
+// permuted alike in both operands.  Second product: 32 columns of Y at a time, MMA i multiplying with rows
+// 8(g / 2) + 2i + g % 2 of B, which leaves lane (g, t) with eight consecutive columns of rows g and g + 8.
+template <int R, bool F32>
+__global__ void __launch_bounds__(FEW_THREADS)
+mwu_adapters_few_kernel(const Params p) {
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ Finder f;
+    Few<R, F32> *sm = reinterpret_cast<Few<R, F32> *>(smem_raw);
+    constexpr int TERMS = Few<R, F32>::TERMS;
+    // Beside the tile kernel: that one has waited for what came before it, so the inputs are there; its own rows are others than these.
+    if (!p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int c = (int)cluster_rank(), clusters = (int)gridDim.x / FEW_CTAS;
+    const int per = (p.segments + FEW_THREADS - 1) / FEW_THREADS;
+    int first;
+    const int total = count_items<true, FEW_THREADS>(p, &f, per, first);
+    if (total < 0 && blockIdx.x == 0 && tid == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_BOUNDS);
+    const int k_chunks = (p.cols + 31) / 32, n_groups = (p.rows + 31) / 32;
+    const int kc0 = (int)((long long)k_chunks * c / FEW_CTAS), kc1 = (int)((long long)k_chunks * (c + 1) / FEW_CTAS);
+    const int ng0 = (int)((long long)n_groups * c / FEW_CTAS), ng1 = (int)((long long)n_groups * (c + 1) / FEW_CTAS);
+
+    for (int item = (int)blockIdx.x / FEW_CTAS; item < total; item += clusters) {
+        __syncthreads();
+        find_item<true>(p, &f, per, first, item);
+        __syncthreads();
+        const int row0 = f.row0, count = f.count, a = f.adapter;
+        if (a < 0) {
+            copy_rows<F32>(p, row0, count, ng0 * 32, min(p.rows, ng1 * 32), tid, FEW_THREADS);
+            continue;
+        }
+        // ---- T = X . A^T over this CTA's slice of cols ----
+        float acc[R / 8][4];
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+        const __nv_bfloat16 *x0 = p.X + (long long)(row0 + g) * p.ldx + 8 * t, *x1 = x0 + 8 * p.ldx;
+        const __nv_bfloat16 *a0 = p.A + (long long)a * p.a_stride + (long long)g * p.lda + 8 * t;
+        for (int ch = kc0 + warp; ch < kc1; ch += FEW_THREADS / 32) {
+            const int k = ch * 32, valid = p.cols - k - 8 * t;
+            const uint4 u = load8(x0 + k, g < count ? valid : 0), v = load8(x1 + k, g + 8 < count ? valid : 0);
+#pragma unroll
+            for (int i = 0; i < R / 8; ++i) {
+                const uint4 w = load8(a0 + (long long)(8 * i) * p.lda + k, 8 * i + g < p.rank ? valid : 0);
+                mma_16816(acc[i], u.x, v.x, u.y, v.y, w.x, w.y);
+                mma_16816(acc[i], u.z, v.z, u.w, v.w, w.z, w.w);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i) {
+            *reinterpret_cast<float2 *>(&sm->red[warp][g][8 * i + 2 * t]) = make_float2(acc[i][0], acc[i][1]);
+            *reinterpret_cast<float2 *>(&sm->red[warp][g + 8][8 * i + 2 * t]) = make_float2(acc[i][2], acc[i][3]);
+        }
+        __syncthreads();
+        for (int e = tid; e < 16 * R; e += FEW_THREADS) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < FEW_THREADS / 32; ++w) s += (&sm->red[w][0][0])[e];
+            (&sm->part[0][0])[e] = s;
+        }
+        cluster_arrive();
+        cluster_wait();
+        // ---- the cluster's sum, scaled, as bf16 terms ----
+        const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
+        for (int e = tid; e < 16 * R; e += FEW_THREADS) {
+            float s = 0.f;
+#pragma unroll
+            for (int o = 0; o < FEW_CTAS; ++o) s += remote_f32(smem_u32(&(&sm->part[0][0])[e]), (unsigned)o);
+            s *= scale;
+#pragma unroll
+            for (int q = 0; q < TERMS; ++q) {
+                const __nv_bfloat16 h = __float2bfloat16_rn(s);
+                sm->T[q][e / R][e % R] = h;
+                s -= __bfloat162float(h);
+            }
+        }
+        cluster_arrive();                                   // the others' sums have been read; waited for below
+        __syncthreads();
+        // ---- Y = Y0 + T . B^T over this CTA's slice of rows ----
+        const __nv_bfloat16 *b0 = p.B + (long long)a * p.b_stride + 4 * t;
+        for (int grp = ng0 + warp; grp < ng1; grp += FEW_THREADS / 32) {
+            const int n0 = grp * 32;
+            float d[4][4];
+            uint2 w[4][R / 16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
+#pragma unroll
+                for (int s = 0; s < R / 16; ++s) w[i][s] = load4(b0 + (long long)n * p.ldb + 16 * s, n < p.rows ? p.rank - 16 * s - 4 * t : 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i][j] = 0.f;
+            }
+#pragma unroll
+            for (int s = 0; s < R / 16; ++s)
+#pragma unroll
+                for (int q = TERMS - 1; q >= 0; --q) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(&sm->T[q][g][16 * s + 4 * t]);
+                    const uint2 v = *reinterpret_cast<const uint2 *>(&sm->T[q][g + 8][16 * s + 4 * t]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma_16816(d[i], u.x, v.x, u.y, v.y, w[i][s].x, w[i][s].y);
+                }
+            const int n = n0 + 8 * t, left = p.rows - n;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (g + 8 * h >= count || left <= 0) continue;
+                const long long at = (long long)(row0 + g + 8 * h) * p.ldy + n;
+                if (F32) {
+                    float *y = reinterpret_cast<float *>(p.Y) + at;
+                    const float *y0 = reinterpret_cast<const float *>(p.Y0) + at;
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        if (left >= 2 * i + 4) {
+                            float4 b = p.Y0 ? *reinterpret_cast<const float4 *>(y0 + 2 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            b.x += d[i][2 * h]; b.y += d[i][2 * h + 1]; b.z += d[i + 1][2 * h]; b.w += d[i + 1][2 * h + 1];
+                            *reinterpret_cast<float4 *>(y + 2 * i) = b;
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (2 * i + j < left) y[2 * i + j] = (p.Y0 ? y0[2 * i + j] : 0.f) + d[i + j / 2][2 * h + j % 2];
+                        }
+                    }
+                } else {
+                    __nv_bfloat16 *y = reinterpret_cast<__nv_bfloat16 *>(p.Y) + at;
+                    const __nv_bfloat16 *y0 = reinterpret_cast<const __nv_bfloat16 *>(p.Y0) + at;
+                    if (left >= 8) {
+                        const uint4 b = p.Y0 ? *reinterpret_cast<const uint4 *>(y0) : make_uint4(0, 0, 0, 0);
+                        const unsigned in[4] = {b.x, b.y, b.z, b.w};
+                        unsigned out[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const __nv_bfloat162 o = __floats2bfloat162_rn(__uint_as_float(in[i] << 16) + d[i][2 * h],
+                                                                           __uint_as_float(in[i] & 0xffff0000u) + d[i][2 * h + 1]);
+                            out[i] = *reinterpret_cast<const unsigned *>(&o);
+                        }
+                        *reinterpret_cast<uint4 *>(y) = make_uint4(out[0], out[1], out[2], out[3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j < left) y[j] = __float2bfloat16_rn((p.Y0 ? __bfloat162float(y0[j]) : 0.f) + d[j / 2][2 * h + j % 2]);
+                    }
+                }
+            }
+        }
+        cluster_wait();
+    }
+    if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");      // what comes behind this kernel comes behind both
+}
+
+// ------------------------------------------------------------------------------------------
+// many rows
+// ------------------------------------------------------------------------------------------
+// A stage of the first product: 128 rows x 64 columns of X and R x 64 of A.  A chunk of the second: 128 rows x 128 bytes of Y0
+// (64 columns of bf16, 32 of fp32) and as many rows of B.  Two rings, so that the first chunks of Y0 and B come in while T is still being added up.
+template <int R, bool F32>
+struct TileCfg {
+    static constexpr int TERMS = F32 ? 3 : 2;
+    static constexpr int CW = F32 ? 32 : 64;                // columns of Y in a chunk
+    static constexpr int BLOCKS = R > 64 ? 2 : 1;           // 64 ranks to a 128-byte row
+    static constexpr int ROWS_BYTES = 128 * 128;
+    static constexpr int IN_SLOT = ROWS_BYTES + (R < 64 ? 8192 : R * 128);
+    static constexpr int OUT_SLOT = ROWS_BYTES + (F32 ? 4096 : 8192) * BLOCKS;
+    static constexpr int T_BYTES = TERMS * BLOCKS * ROWS_BYTES;
+    static constexpr int IN_SLOTS = R > 64 ? (F32 ? 2 : 3) : 4;
+    static constexpr int OUT_SLOTS = R > 64 ? 2 : 3;
+    static constexpr int SMEM = T_BYTES + IN_SLOTS * IN_SLOT + OUT_SLOTS * OUT_SLOT;
+    static_assert(IN_SLOTS * IN_SLOT >= 128 * R * 4, "the ring of the first product takes its sums afterwards");
+};
+
+struct TileSmem {
+    unsigned long long full1[4], empty1[4], full2[3], empty2[3], tfull1[2], tempty1[2], tfull2[2], tempty2[2], drain;
+    unsigned tmem_base;
+    int abort, drain_abort;
+    Finder f;
+};
+
+template <int R, bool F32>
+constexpr int tile_smem() { return 1024 + TileCfg<R, F32>::SMEM + (int)sizeof(TileSmem); }
+// This kernel's clusters hold tensor memory while their CTAs wait for one another.  Were a CTA of another such kernel (on another
+// stream) on the same SM, each could hold what the other waits for; with this much shared memory none fits beside it.
+constexpr int TILE_LEAST_SMEM = 196 * 1024;
+
+__device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+__device__ __forceinline__ unsigned cluster_size() {
+    unsigned n;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    return n;
+}
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+template <int R, bool F32>
+__global__ void __launch_bounds__(TILE_THREADS, 1)
+mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a,
+                         const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y0,
+                         const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ Params p) {
+    using C = TileCfg<R, F32>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *sT = smem_raw + smem_pad_1024(smem_raw);
+    unsigned char *s1 = sT + C::T_BYTES, *s2 = s1 + C::IN_SLOTS * C::IN_SLOT;
+    TileSmem *sm = reinterpret_cast<TileSmem *>(s2 + C::OUT_SLOTS * C::OUT_SLOT);
+    volatile int *abort = &sm->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ctas = (int)cluster_size(), c = (int)cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::IN_SLOTS; ++s) {
+            mbar_init(smem_u32(&sm->full1[s]), 1);
+            mbar_init(smem_u32(&sm->empty1[s]), 1);
+        }
+        for (int s = 0; s < C::OUT_SLOTS; ++s) {
+            mbar_init(smem_u32(&sm->full2[s]), 1);
+            mbar_init(smem_u32(&sm->empty2[s]), 4);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&sm->tfull1[b]), 1);
+            mbar_init(smem_u32(&sm->tempty1[b]), 8);
+            mbar_init(smem_u32(&sm->tfull2[b]), 1);
+            mbar_init(smem_u32(&sm->tempty2[b]), 4);
+        }
+        mbar_init(smem_u32(&sm->drain), 1);
+        sm->abort = 0;
+        sm->drain_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&sm->tmem_base), 512);
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel for few rows works beside this one
+    }
+    const int per = (p.segments + TILE_THREADS - 1) / TILE_THREADS;
+    int first;
+    const int total = count_items<false, TILE_THREADS>(p, &sm->f, per, first);
+    const int item = (int)blockIdx.x / ctas;
+    if (item < total) find_item<false>(p, &sm->f, per, first, item);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
+    const bool work = item < total;                         // the whole cluster alike
+    const int row0 = work ? sm->f.row0 : 0, count = work ? sm->f.count : 0, a = work ? sm->f.adapter : -1;
+    const int k_all = (p.cols + 63) / 64, n_all = (p.rows + C::CW - 1) / C::CW;
+    const int ks0 = (int)((long long)k_all * c / ctas), ks1 = (int)((long long)k_all * (c + 1) / ctas);
+    const int nc0 = (int)((long long)n_all * c / ctas), nc1 = (int)((long long)n_all * (c + 1) / ctas);
+    const int bands = (count + 31) / 32;                    // runs of 32 rows that hold any
+    constexpr int PIECE = 8;                                // stages between two sums of T (512 products)
+
+    if (work && a < 0) {
+        copy_rows<F32>(p, row0, count, nc0 * C::CW, min(p.rows, nc1 * C::CW), threadIdx.x, TILE_THREADS);
+    } else if (work && warp == 0) {
+        // ---------------- TMA producer ----------------
+        bool ok = true;
+        int n1 = 0, n2 = 0;                                 // stages and chunks asked for so far
+        for (int ks = ks0; ks < ks1; ++ks, ++n1) {
+            const int s = n1 % C::IN_SLOTS;
+            ok = warp_wait_spin(smem_u32(&sm->empty1[s]), ((unsigned)(n1 / C::IN_SLOTS) & 1u) ^ 1u, abort);
+            if (!ok) break;
+            if (elect_one()) {
+                const unsigned bar = smem_u32(&sm->full1[s]), dst = smem_u32(s1 + s * C::IN_SLOT);
+                mbar_expect_tx(bar, (unsigned)(bands * 4096 + R * 128));
+                for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_x, bar, ks * 64, row0 + 32 * b);
+                tma_load_3d(dst + C::ROWS_BYTES, &tm_a, bar, ks * 64, 0, a);
+            }
+            __syncwarp();
+        }
+        cluster_arrive();
+        bool waited = false;
+        for (int i = nc0; i < nc1 && ok; ++i, ++n2) {
+            const int s = n2 % C::OUT_SLOTS;
+            if (n2 == C::OUT_SLOTS) {                       // the first slots are free; the others need T
+                cluster_wait();
+                cluster_arrive();
+                cluster_wait();
+                waited = true;
+            }
+            ok = warp_wait_spin(smem_u32(&sm->empty2[s]), ((unsigned)(n2 / C::OUT_SLOTS) & 1u) ^ 1u, abort);
+            if (!ok) break;
+            if (elect_one()) {
+                const unsigned bar = smem_u32(&sm->full2[s]), dst = smem_u32(s2 + s * C::OUT_SLOT);
+                mbar_expect_tx(bar, (unsigned)((p.Y0 ? bands * 4096 : 0) + C::CW * 128 * C::BLOCKS));
+                for (int q = 0; q < C::BLOCKS; ++q)
+                    tma_load_3d(dst + C::ROWS_BYTES + q * C::CW * 128, &tm_b, bar, 64 * q, i * C::CW, a);
+                if (p.Y0)
+                    for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_y0, bar, i * C::CW, row0 + 32 * b);
+            }
+            __syncwarp();
+        }
+        if (!waited) {
+            cluster_wait();
+            cluster_arrive();
+            cluster_wait();
+        }
+        // a wait ran out: the loads in flight land before this CTA leaves
+        if (__any_sync(0xffffffffu, *abort)) {
+            for (int s = 0; s < C::IN_SLOTS; ++s)
+                if (n1 > s) mbar_wait(smem_u32(&sm->full1[s]), (unsigned)((n1 - s - 1) / C::IN_SLOTS) & 1u, &sm->drain_abort);
+            for (int s = 0; s < C::OUT_SLOTS; ++s)
+                if (n2 > s) mbar_wait(smem_u32(&sm->full2[s]), (unsigned)((n2 - s - 1) / C::OUT_SLOTS) & 1u, &sm->drain_abort);
+            __syncwarp();
+        }
+    } else if (work && warp == 1) {
+        // ---------------- MMA issuer ----------------
+        bool ok = true;
+        int n = 0;
+        unsigned use = 0;
+        for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
+            ok = warp_wait_spin(smem_u32(&sm->tempty1[use & 1u]), ((use >> 1) & 1u) ^ 1u, abort);
+            if (!ok) break;
+            tc_fence_after();
+            const int k1 = min(ks1, k0 + PIECE);
+            for (int ks = k0; ks < k1; ++ks, ++n) {
+                const int s = n % C::IN_SLOTS;
+                ok = warp_wait_spin(smem_u32(&sm->full1[s]), (unsigned)(n / C::IN_SLOTS) & 1u, abort);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const unsigned long long xd = make_desc(smem_u32(s1 + s * C::IN_SLOT));
+                    const unsigned long long ad = make_desc(smem_u32(s1 + s * C::IN_SLOT + C::ROWS_BYTES));
+#pragma unroll
+                    for (int k4 = 0; k4 < 4; ++k4)
+                        umma_bf16(tmem_base + (use & 1u) * R, xd + 2ull * k4, ad + 2ull * k4, make_idesc(R), (ks > k0 || k4) ? 1u : 0u);
+                    umma_commit(smem_u32(&sm->empty1[s]));
+                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            if (elect_one()) umma_commit(smem_u32(&sm->tfull1[use & 1u]));
+            __syncwarp();
+        }
+        cluster_arrive();
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();                                     // T of all rows is here, as bf16 terms
+        fence_proxy_async_all();
+        n = 0;
+        for (int i = nc0; ok && i < nc1; ++i, ++n) {
+            const int s = n % C::OUT_SLOTS;
+            const unsigned buf = (unsigned)n & 1u;
+            ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((unsigned)(n >> 1) & 1u) ^ 1u, abort) &&
+                 warp_wait_spin(smem_u32(&sm->full2[s]), (unsigned)(n / C::OUT_SLOTS) & 1u, abort);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                unsigned acc = 0;
+#pragma unroll
+                for (int q = C::TERMS - 1; q >= 0; --q)     // the smallest term first
+#pragma unroll
+                    for (int j = 0; j < R / 16; ++j) {
+                        const unsigned long long td = make_desc(smem_u32(sT + (q * C::BLOCKS + j / 4) * C::ROWS_BYTES));
+                        const unsigned long long bd = make_desc(smem_u32(s2 + s * C::OUT_SLOT + C::ROWS_BYTES + (j / 4) * C::CW * 128));
+                        umma_bf16(tmem_base + 256u + buf * 64u, td + 2ull * (j % 4), bd + 2ull * (j % 4), make_idesc(C::CW), acc);
+                        acc = 1;
+                    }
+                umma_commit(smem_u32(&sm->tfull2[buf]));
+            }
+            __syncwarp();
+        }
+        // everything this thread issued must have retired before tensor memory is freed
+        if (elect_one()) umma_commit(smem_u32(&sm->drain));
+        __syncwarp();
+        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort);
+        __syncwarp();
+    } else if (work) {
+        const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane, tid = threadIdx.x - 64;
+        bool ok = true;
+        // ---------------- T of this CTA's slice, to shared memory ----------------
+        constexpr int MINE = R >= 64 ? R / 2 : R;           // columns of T a warp takes (up to 32 ranks: the first four warps)
+        constexpr int LD = MINE < 32 ? 16 : 32;
+        const int col0 = R >= 64 ? half * MINE : 0;
+        float t[MINE];
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) t[j] = 0.f;
+        unsigned use = 0;
+        for (int k0 = ks0; k0 < ks1; k0 += PIECE, ++use) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull1[use & 1u]), (use >> 1) & 1u, abort));
+            if (!ok) break;
+            tc_fence_after();
+            if (R >= 64 || half == 0) {
+#pragma unroll
+                for (int q = 0; q < MINE / LD; ++q) {
+                    unsigned v[LD];
+                    const unsigned at = tmem_base + ((unsigned)(quarter * 32) << 16) + (use & 1u) * R + (unsigned)(col0 + q * LD);
+                    if constexpr (LD == 16) tmem_ld16(at, v);
+                    else tmem_ld32(at, v);
+#pragma unroll
+                    for (int j = 0; j < LD; ++j) t[q * LD + j] += __uint_as_float(v[j]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm->tempty1[use & 1u]));
+        }
+        // four ranks of a row to 16 bytes, rows next to one another.  (The first product's ring is free: its last MMA has been waited for.)
+        float4 *part = reinterpret_cast<float4 *>(s1);
+        if (R >= 64 || half == 0) {
+#pragma unroll
+            for (int j = 0; j < MINE / 4; ++j)
+                part[(col0 / 4 + j) * 128 + row] = make_float4(t[4 * j], t[4 * j + 1], t[4 * j + 2], t[4 * j + 3]);
+        }
+        cluster_arrive();
+        cluster_wait();
+        // ---------------- this CTA's share of the rows: added up, scaled, split, given to all ----------------
+        const int r0 = 128 * c / ctas, nr = 128 * (c + 1) / ctas - r0;
+        const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
+        for (int e = tid; e < nr * (R / 4); e += 256) {
+            const int r = r0 + e % nr, q4 = e / nr;
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int o = 0; o < ctas; ++o) {
+                unsigned at;
+                float4 v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(part + q4 * 128 + r)), "r"(o));
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            float f[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+            const unsigned place = (unsigned)(q4 / 16) * C::ROWS_BYTES + (r >> 3) * 1024u + (r & 7) * 128u +
+                                   ((((unsigned)q4 >> 1 & 7u) ^ (r & 7)) << 4) + (q4 & 1) * 8u;
+#pragma unroll
+            for (int q = 0; q < C::TERMS; ++q) {
+                unsigned w[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+                    w[j] = *reinterpret_cast<const unsigned *>(&h);
+                    f[2 * j] -= __low2float(h);
+                    f[2 * j + 1] -= __high2float(h);
+                }
+                for (int o = 0; o < ctas; ++o) {
+                    unsigned at;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                                 : "=r"(at) : "r"(smem_u32(sT) + (unsigned)(q * C::BLOCKS * C::ROWS_BYTES) + place), "r"(o));
+                    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w[0]), "r"(w[1]) : "memory");
+                }
+            }
+        }
+        fence_proxy_async_all();
+        cluster_arrive();
+        cluster_wait();
+        // ---------------- chunks of Y: four warps take the even ones, four the odd ones ----------------
+        const int rows_here = min(32, max(0, count - quarter * 32));
+        for (int i = nc0 + half, n = half; ok && i < nc1; i += 2, n += 2) {
+            const int s = n % C::OUT_SLOTS;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), (unsigned)(n >> 1) & 1u, abort) &&
+                                             mbar_wait(smem_u32(&sm->full2[s]), (unsigned)(n / C::OUT_SLOTS) & 1u, abort));
+            if (!ok) break;
+            tc_fence_after();
+            unsigned v[C::CW / 32][32];
+#pragma unroll
+            for (int q = 0; q < C::CW / 32; ++q)
+                tmem_ld32(tmem_base + ((unsigned)(quarter * 32) << 16) + 256u + (unsigned)(half * 64 + q * 32), v[q]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm->tempty2[half]));
+            unsigned char *box = s2 + s * C::OUT_SLOT + quarter * 4096;
+            const int n0 = i * C::CW;
+            if (rows_here > 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + ((j ^ (lane & 7)) << 4));
+                    uint4 y = p.Y0 ? *at : make_uint4(0, 0, 0, 0);
+                    if (F32) {
+                        y.x = __float_as_uint(__uint_as_float(y.x) + __uint_as_float(v[0][4 * j]));
+                        y.y = __float_as_uint(__uint_as_float(y.y) + __uint_as_float(v[0][4 * j + 1]));
+                        y.z = __float_as_uint(__uint_as_float(y.z) + __uint_as_float(v[0][4 * j + 2]));
+                        y.w = __float_as_uint(__uint_as_float(y.w) + __uint_as_float(v[0][4 * j + 3]));
+                    } else {
+                        unsigned w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int e = 8 * j + 2 * q;
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[q] << 16) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32]),
+                                                                           __uint_as_float(w[q] & 0xffff0000u) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32 + 1]));
+                            w[q] = *reinterpret_cast<const unsigned *>(&h);
+                        }
+                        y = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    *at = y;
+                }
+                // Whole boxes, clipped at the last column by the map, which clips a store at 16 bytes only.
+                if (rows_here == 32 && (n0 + C::CW <= p.rows || p.rows % (C::CW / 8) == 0)) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&tm_y, smem_u32(box), n0, row0 + quarter * 32);
+                        bulk_commit();
+                        bulk_wait_read();
+                    }
+                } else {                                    // the rows behind are another segment's, the columns behind the caller's
+                    __syncwarp();
+                    for (int b = 0; b < rows_here; b += 4) {
+                        const int r = b + (lane >> 3), j = lane & 7, left = p.rows - n0 - j * (C::CW / 8);
+                        if (r < rows_here && left > 0) {
+                            const uint4 y = *reinterpret_cast<const uint4 *>(box + r * 128 + ((j ^ (r & 7)) << 4));
+                            const long long at = (long long)(row0 + quarter * 32 + r) * p.ldy + n0 + j * (C::CW / 8);
+                            if (left >= C::CW / 8) {
+                                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.Y) + at * (F32 ? 4 : 2)) = y;
+                            } else {
+                                const unsigned w[4] = {y.x, y.y, y.z, y.w};
+                                for (int e = 0; e < left; ++e) {
+                                    if (F32) reinterpret_cast<unsigned *>(p.Y)[at + e] = e == 0 ? w[0] : e == 1 ? w[1] : w[2];
+                                    else {
+                                        const unsigned u = e < 2 ? w[0] : e < 4 ? w[1] : e < 6 ? w[2] : w[3];
+                                        reinterpret_cast<unsigned short *>(p.Y)[at + e] = (unsigned short)(e & 1 ? u >> 16 : u);
+                                    }
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm->empty2[s]));
+        }
+        if (lane == 0) bulk_wait_all();
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (*abort) atomicOr(p.dev_status, (unsigned)MWU_DEV_TIMEOUT);
+        if (total < 0 && blockIdx.x == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_BOUNDS);
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------
+template <int R, bool F32>
+static cudaError_t launch_few(const Params &p, int sm_count, cudaStream_t st) {
+    auto kern = mwu_adapters_few_kernel<R, F32>;
+    const size_t smem = sizeof(Few<R, F32>);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    // a cluster for every 16 rows that there may be in such segments, as far as four CTAs an SM go; more items are taken in turn
+    long long items = (long long)p.segments + p.M / 16;
+    if (items > 2ll * p.segments) items = 2ll * p.segments;
+    if (items > p.M) items = p.M;
+    const long long most = 4ll * sm_count / FEW_CTAS;
+    count_launch();
+    return launch_chained(kern, dim3((unsigned)(FEW_CTAS * (items < most ? items : most))), dim3(FEW_THREADS), smem, st, FEW_CTAS, p);
+}
+
+static bool encode(CUtensorMap *tm, const void *ptr, bool fp32, int64_t inner, int64_t rows, int64_t ld, int box_rows, int64_t n, int64_t stride) {
+    const int64_t size = fp32 ? 4 : 2;
+    const cuuint64_t gdim[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)n};
+    const cuuint64_t gstride[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(stride * size)};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return get_encode_fn()(tm, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n ? 3 : 2, const_cast<void *>(ptr),
+                           gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int R, bool F32>
+static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
+    auto kern = mwu_adapters_tile_kernel<R, F32>;
+    using C = TileCfg<R, F32>;
+    constexpr int smem = tile_smem<R, F32>() > TILE_LEAST_SMEM ? tile_smem<R, F32>() : TILE_LEAST_SMEM;
+    static_assert(smem <= 232448, "adapter tile kernel: shared memory above 227 KB");
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MWU_ERR_CUDA;
+    if (!get_encode_fn()) return MWU_ERR_CUDA;
+    CUtensorMap tm_x, tm_a, tm_b, tm_y0, tm_y;
+    if (!encode(&tm_x, p.X, false, p.cols, p.M, p.ldx, 32, 0, 0) || !encode(&tm_a, p.A, false, p.cols, p.rank, p.lda, R, p.adapters, p.a_stride) ||
+        !encode(&tm_b, p.B, false, p.rank, p.rows, p.ldb, C::CW, p.adapters, p.b_stride) || !encode(&tm_y, p.Y, F32, p.rows, p.M, p.ldy, 32, 0, 0) ||
+        !encode(&tm_y0, p.Y0 ? p.Y0 : p.Y, F32, p.rows, p.M, p.ldy, 32, 0, 0))
+        return MWU_ERR_CUDA;
+    // Longer segments than FEW_ROWS have an item for every 128 rows and one that is not full.  The cluster is as large as keeps
+    // what is to be expected (half of the segments full ones) in one round; any size gives every row its adapter.
+    const long long longer = p.M / (FEW_ROWS + 1), some = longer < p.segments ? longer : p.segments;
+    const long long most = p.M / 128 + some, expected = (p.M + 127) / 128 + (some < p.M / 256 ? some : p.M / 256);
+    long long ctas = sm_count / expected;
+    ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
+    count_launch();
+    return launch_chained(kern, dim3((unsigned)(most * ctas)), dim3(TILE_THREADS), smem, st, (int)ctas, tm_x, tm_a, tm_b, tm_y0, tm_y, p) ==
+                   cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+}
+
+template <int R, bool F32>
+static int launch_both(Params p, int sm_count, cudaStream_t st) {
+    if (p.M > FEW_ROWS) {
+        const int rc = launch_tile<R, F32>(p, sm_count, st);
+        if (rc != MWU_OK) return rc;
+        p.beside = 1;
+    }
+    return launch_few<R, F32>(p, sm_count, st) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+}
+
+template <bool F32>
+static int launch_rank(const Params &p, int sm_count, cudaStream_t st) {
+    if (p.rank <= 16) return launch_both<16, F32>(p, sm_count, st);
+    if (p.rank <= 32) return launch_both<32, F32>(p, sm_count, st);
+    if (p.rank <= 64) return launch_both<64, F32>(p, sm_count, st);
+    return launch_both<128, F32>(p, sm_count, st);
+}
+
+}  // namespace adapters
+}  // namespace mwu
+
+extern "C" int mwu_adapters_add(int64_t adapters, int64_t rank, int64_t rows, int64_t cols, const void *A, int64_t lda, int64_t a_stride,
+                                const void *B, int64_t ldb, int64_t b_stride, const float *scale, int64_t segments,
+                                const int32_t *offsets, const int32_t *which, const void *X, int64_t M, int64_t ldx, const void *Y0,
+                                void *Y, int64_t ldy, int32_t y_dtype, uint32_t *dev_status, void *cuda_stream) {
+    using namespace mwu;
+    if (!A || !B || !offsets || !which || !X || !Y || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if (y_dtype != 0 && y_dtype != 1) return MWU_ERR_INVALID_ARG;
+    if (adapters <= 0 || adapters >= (int64_t(1) << 31) || segments < 0 || segments > MWU_MAX_SEGMENTS) return MWU_ERR_SHAPE;
+    if (rank <= 0 || rank > MWU_MAX_RANK || rows <= 0 || cols <= 0 || lda < cols || ldb < rank || ldx < cols || ldy < rows) return MWU_ERR_SHAPE;
+    if (rows > MWU_MAX_GROUPED_SIDE || cols > MWU_MAX_GROUPED_SIDE || M >= (int64_t(1) << 31) - 256) return MWU_ERR_SHAPE;
+    if (lda >= (int64_t(1) << 31) || ldb >= (int64_t(1) << 31) || ldx >= (int64_t(1) << 31) || ldy >= (int64_t(1) << 31)) return MWU_ERR_SHAPE;
+    if (a_stride < rank * lda || b_stride < rows * ldb || a_stride >= (int64_t(1) << 38) || b_stride >= (int64_t(1) << 38)) return MWU_ERR_SHAPE;
+    if (!aligned_to(A, 16) || !aligned_to(B, 16) || !aligned_to(X, 16) || !aligned_to(Y0, 16) || !aligned_to(Y, 16) || !aligned_to(scale, 4) ||
+        !aligned_to(offsets, 4) || !aligned_to(which, 4) || !aligned_to(dev_status, 4) || lda % 8 != 0 || ldb % 8 != 0 || ldx % 8 != 0 ||
+        a_stride % 8 != 0 || b_stride % 8 != 0 || ldy % (y_dtype ? 4 : 8) != 0)
+        return MWU_ERR_ALIGNMENT;
+    int sm_count = 0;
+    const int rc = check_device(&sm_count);
+    if (rc != MWU_OK) return rc;
+    if (M == 0 || segments == 0) return MWU_OK;
+    adapters::Params p = {};
+    p.A = (const __nv_bfloat16 *)A; p.B = (const __nv_bfloat16 *)B; p.X = (const __nv_bfloat16 *)X;
+    p.lda = lda; p.a_stride = a_stride; p.ldb = ldb; p.b_stride = b_stride; p.ldx = ldx; p.ldy = ldy;
+    p.scale = scale; p.offsets = offsets; p.which = which; p.Y0 = Y0; p.Y = Y;
+    p.adapters = (int)adapters; p.rank = (int)rank; p.rows = (int)rows; p.cols = (int)cols; p.segments = (int)segments; p.M = (int)M;
+    p.dev_status = dev_status;
+    return y_dtype ? adapters::launch_rank<true>(p, sm_count, (cudaStream_t)cuda_stream)
+                   : adapters::launch_rank<false>(p, sm_count, (cudaStream_t)cuda_stream);
+}

@@ -1,4 +1,4 @@
-"""Arguments that the grouped products refuse, before any CUDA call (runs without a GPU)."""
+"""Arguments that the grouped products and the adapters refuse, before any CUDA call (runs without a GPU)."""
 import ctypes
 
 import pytest
@@ -50,3 +50,31 @@ def test_what_is_allowed_reaches_the_device_check():
         assert getattr(B.lib(), name)(*LINES.values()) in late
         assert getattr(B.lib(), name)(*dict(LINES, groups=B.MWU_MAX_GROUPS, M=1, dtype=1).values()) in late
     assert B.lib().mwu_gemm_grouped_dw(*GRAD.values()) in late
+
+
+ADAPTERS = dict(adapters=4, rank=16, rows=64, cols=128, A=P, lda=128, a_stride=16 * 128, B=P, ldb=16, b_stride=64 * 16, scale=P, segments=3,
+                offsets=P, which=P, X=P, M=100, ldx=128, Y0=P, Y=P, ldy=64, dtype=0, status=P, stream=None)
+ODD = ctypes.c_void_p((1 << 20) + 8)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(A=None), INVALID), (dict(B=None), INVALID), (dict(offsets=None), INVALID), (dict(which=None), INVALID), (dict(X=None), INVALID),
+    (dict(Y=None), INVALID), (dict(status=None), INVALID), (dict(M=-1), INVALID), (dict(dtype=2), INVALID),
+    (dict(adapters=0), SHAPE), (dict(adapters=1 << 31), SHAPE), (dict(segments=-1), SHAPE), (dict(segments=B.MWU_MAX_SEGMENTS + 1), SHAPE),
+    (dict(rank=0), SHAPE), (dict(rank=B.MWU_MAX_RANK + 1, ldb=256, a_stride=1 << 20, b_stride=1 << 20), SHAPE), (dict(rows=0), SHAPE),
+    (dict(cols=0), SHAPE), (dict(rows=B.MWU_MAX_GROUPED_SIDE + 1), SHAPE), (dict(M=2 ** 31), SHAPE), (dict(lda=120), SHAPE), (dict(ldb=8), SHAPE),
+    (dict(ldx=120), SHAPE), (dict(ldy=56), SHAPE), (dict(a_stride=16 * 128 - 8), SHAPE), (dict(b_stride=64 * 16 - 8), SHAPE),
+    (dict(lda=132, a_stride=16 * 132), ALIGNMENT), (dict(ldb=20, b_stride=64 * 20), ALIGNMENT), (dict(ldx=132), ALIGNMENT),
+    (dict(a_stride=16 * 128 + 4), ALIGNMENT), (dict(b_stride=64 * 16 + 4), ALIGNMENT), (dict(ldy=68), ALIGNMENT), (dict(ldy=66, dtype=1), ALIGNMENT),
+    (dict(A=ODD), ALIGNMENT), (dict(B=ODD), ALIGNMENT), (dict(X=ODD), ALIGNMENT), (dict(Y0=ODD), ALIGNMENT), (dict(Y=ODD), ALIGNMENT),
+    (dict(scale=ctypes.c_void_p((1 << 20) + 2)), ALIGNMENT), (dict(which=ctypes.c_void_p((1 << 20) + 2)), ALIGNMENT)])
+def test_adapters_refuse(change, want):
+    assert B.lib().mwu_adapters_add(*dict(ADAPTERS, **change).values()) == want
+
+
+def test_adapters_that_are_allowed_reach_the_device_check():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the pointers are made up")
+    for change in (dict(), dict(Y0=None, scale=None), dict(rank=B.MWU_MAX_RANK, ldb=128, a_stride=128 * 128, b_stride=64 * 128), dict(dtype=1, ldy=68)):
+        assert B.lib().mwu_adapters_add(*dict(ADAPTERS, **change).values()) in (B.MWU_ERR_CUDA, B.MWU_ERR_UNSUPPORTED_DEVICE)
