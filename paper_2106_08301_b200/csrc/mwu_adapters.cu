@@ -26,9 +26,10 @@ EncodeTiledFn get_encode_fn();          // mwu_gemm.cu
 namespace adapters {
 using namespace gemm;
 
-constexpr int FEW_ROWS = 32;            // rows of a segment that the first kernel takes
-constexpr int FEW_CTAS = 8;
+constexpr int FEW_ROWS = 32;            // rows of a segment that the first kernel takes,
+constexpr int FEW_IN_ALL = 256;         // and rows of a call that it takes whatever its segments, sorted by adapter
 constexpr int FEW_THREADS = 256;
+static_assert(FEW_IN_ALL == FEW_THREADS, "a thread sorts one row");
 constexpr int TILE_THREADS = 320;
 
 struct Params {
@@ -39,6 +40,7 @@ struct Params {
     const void *Y0;
     void *Y;
     int adapters, rank, rows, cols, segments, M;
+    int few_rows;                       // FEW_ROWS, or as many as may be
     int beside;                         // the few-rows kernel runs beside the tile kernel launched before it
     unsigned *dev_status;
 };
@@ -53,7 +55,7 @@ struct Finder {
 
 // rows of a segment that lie in one work item, or 0 where the segment is the other kernel's
 template <bool FEW>
-__device__ __forceinline__ int item_rows(int len) { return (len <= FEW_ROWS) == FEW ? (FEW ? 16 : 128) : 0; }
+__device__ __forceinline__ int item_rows(const Params &p, int len) { return (len <= p.few_rows) == FEW ? (FEW ? 16 : 128) : 0; }
 
 // Thread i looks after segments i * per .. of the list; its items are number `first` and on.  Returns how many there are in all,
 // -1 where the list makes no sense.  All threads of the CTA.
@@ -65,7 +67,7 @@ __device__ __forceinline__ int count_items(const Params &p, Finder *f, int per, 
         const int a = __ldg(p.offsets + s), b = __ldg(p.offsets + s + 1), w = __ldg(p.which + s);
         const bool wrong = a < 0 || b < a || b > p.M || w < -1 || w >= p.adapters;
         bad |= wrong;
-        const int unit = wrong ? 0 : item_rows<FEW>(b - a);
+        const int unit = wrong ? 0 : item_rows<FEW>(p, b - a);
         if (unit) mine += (b - a + unit - 1) / unit;
     }
     int upto = mine;
@@ -93,7 +95,7 @@ __device__ __forceinline__ void find_item(const Params &p, Finder *f, int per, i
     if (item < first) return;
     int at = first;
     for (int s = threadIdx.x * per; s < (int)(threadIdx.x + 1) * per && s < p.segments; ++s) {
-        const int a = __ldg(p.offsets + s), len = __ldg(p.offsets + s + 1) - a, unit = item_rows<FEW>(len);
+        const int a = __ldg(p.offsets + s), len = __ldg(p.offsets + s + 1) - a, unit = item_rows<FEW>(p, len);
         const int n = unit ? (len + unit - 1) / unit : 0;
         if (item < at + n) {
             const int r = (item - at) * unit;
@@ -106,23 +108,89 @@ __device__ __forceinline__ void find_item(const Params &p, Finder *f, int per, i
     }
 }
 
-// Y = Y0 (or zeros) for rows without an adapter, columns n0 .. n1 (n0 a multiple of 32), 16 bytes at a time
-template <bool F32>
-__device__ __forceinline__ void copy_rows(const Params &p, int row0, int count, int n0, int n1, int tid, int threads) {
+// A call of few rows in all is worked on adapter by adapter, 16 rows at a time, wherever in the batch they are: 64 tokens of 32
+// adapters read every adapter once, not twice.
+struct Sorter {
+    int key[FEW_THREADS];               // adapter of a row; NOBODY: of no segment
+    int row[FEW_THREADS];               // rows in the order of their adapters
+    int start[FEW_THREADS + 1];         // where an item's rows start in `row`
+    unsigned starts[FEW_THREADS / 32];
+    int counted;
+};
+constexpr int NOBODY = 0x7fffffff;
+
+// returns the number of items, -1 where the list makes no sense.  All threads of the CTA.
+__device__ __forceinline__ int sort_rows(const Params &p, Sorter *o, int per) {
+    const int tid = threadIdx.x;
+    o->key[tid] = NOBODY;
+    if (tid < FEW_THREADS / 32) o->starts[tid] = 0u;
+    if (tid == 0) o->counted = 0;
+    __syncthreads();
+    int bad = 0;
+    for (int s = tid * per; s < (tid + 1) * per && s < p.segments; ++s) {
+        const int a = __ldg(p.offsets + s), b = __ldg(p.offsets + s + 1), w = __ldg(p.which + s);
+        const bool wrong = a < 0 || b < a || b > p.M || w < -1 || w >= p.adapters;
+        bad |= wrong;
+        if (!wrong)
+            for (int r = a; r < b; ++r) o->key[r] = w;
+    }
+    if (__syncthreads_or(bad)) return -1;
+    const int mine = o->key[tid];
+    int less = 0, same = 0;                                 // rows of smaller adapters; of mine, before this one
+    for (int j = 0; j < p.M; j += 4) {
+        const int4 k = *reinterpret_cast<const int4 *>(&o->key[j]);
+        less += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+        same += (k.x == mine && j < tid) + (k.y == mine && j + 1 < tid) + (k.z == mine && j + 2 < tid) + (k.w == mine && j + 3 < tid);
+    }
+    const int at = less + same;
+    const bool counts = mine != NOBODY, first = counts && same % 16 == 0;
+    if (counts) {
+        o->row[at] = tid;
+        atomicAdd(&o->counted, 1);
+    }
+    if (first) atomicOr(&o->starts[at / 32], 1u << (at % 32));
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < FEW_THREADS / 32; ++w) {
+        const unsigned v = o->starts[w];
+        before += __popc(w < at / 32 ? v : (w == at / 32 ? v & ((1u << (at % 32)) - 1u) : 0u));
+        total += __popc(v);
+    }
+    if (first) o->start[before] = at;
+    if (tid == 0) o->start[total] = o->counted;
+    __syncthreads();
+    return total;
+}
+
+// Y = Y0 (or zeros) for rows without an adapter, columns n0 .. n1 (n0 a multiple of 32), 16 bytes at a time, AT_ONCE of them in flight
+template <bool F32, int AT_ONCE, typename RowOf>
+__device__ __forceinline__ void copy_rows(const Params &p, RowOf row_of, int count, int n0, int n1, int tid, int threads) {
     if (p.Y0 == p.Y || n1 <= n0) return;
     constexpr int SIZE = F32 ? 4 : 2, UNIT = 16 / SIZE;
     const unsigned char *from = reinterpret_cast<const unsigned char *>(p.Y0);
     unsigned char *to = reinterpret_cast<unsigned char *>(p.Y);
     const unsigned units = (unsigned)(n1 - n0 + UNIT - 1) / UNIT;
-    for (unsigned e = tid; e < units * (unsigned)count; e += threads) {
-        const unsigned r = e / units;
-        const int n = n0 + (int)(e - r * units) * UNIT;
-        const long long at = ((long long)(row0 + (int)r) * p.ldy + n) * SIZE;
-        if (n + UNIT <= n1) {
-            *reinterpret_cast<uint4 *>(to + at) = from ? *reinterpret_cast<const uint4 *>(from + at) : make_uint4(0, 0, 0, 0);
-        } else {
-            for (int b = 0; b < (n1 - n) * SIZE; b += 2)
-                *reinterpret_cast<unsigned short *>(to + at + b) = from ? *reinterpret_cast<const unsigned short *>(from + at + b) : (unsigned short)0;
+    for (unsigned e0 = tid; e0 < units * (unsigned)count; e0 += AT_ONCE * threads) {
+        uint4 v[AT_ONCE];
+        long long at[AT_ONCE];
+        int left[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const unsigned e = e0 + j * threads, r = e / units;
+            const int n = n0 + (int)(e - r * units) * UNIT;
+            left[j] = e < units * (unsigned)count ? n1 - n : 0;
+            if (left[j] <= 0) continue;
+            at[j] = ((long long)row_of((int)r) * p.ldy + n) * SIZE;
+            v[j] = make_uint4(0, 0, 0, 0);
+            if (from && left[j] >= UNIT) v[j] = *reinterpret_cast<const uint4 *>(from + at[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            if (left[j] >= UNIT) *reinterpret_cast<uint4 *>(to + at[j]) = v[j];
+            else
+                for (int b = 0; b < left[j] * SIZE; b += 2)
+                    *reinterpret_cast<unsigned short *>(to + at[j] + b) = from ? *reinterpret_cast<const unsigned short *>(from + at[j] + b) : (unsigned short)0;
         }
     }
 }
@@ -131,41 +199,43 @@ __device__ __forceinline__ void copy_rows(const Params &p, int row0, int count, 
 // few rows
 // ------------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma_16816(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Loads come first and what lies past the end of a row is cleared afterwards, and only where a row ends: a test that
+// needs the value of one load would hold up the next.
+__device__ __forceinline__ uint4 load8_if(const __nv_bfloat16 *at, bool take) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (take) v = __ldg(reinterpret_cast<const uint4 *>(at));
+    return v;
+}
+__device__ __forceinline__ uint2 load4_if(const __nv_bfloat16 *at, bool take) {
+    uint2 v = make_uint2(0, 0);
+    if (take) v = __ldg(reinterpret_cast<const uint2 *>(at));
+    return v;
 }
 // the first `valid` of a word's two halves of elements e, e + 1
 __device__ __forceinline__ unsigned keep_valid(unsigned w, int e, int valid) {
     return e + 1 < valid ? w : (e < valid ? w & 0xffffu : 0u);
 }
-// eight consecutive elements of a row that has `valid` left from here
-__device__ __forceinline__ uint4 load8(const __nv_bfloat16 *at, int valid) {
-    if (valid <= 0) return make_uint4(0, 0, 0, 0);
-    uint4 v = __ldg(reinterpret_cast<const uint4 *>(at));
-    if (valid < 8) {
-        v.x = keep_valid(v.x, 0, valid);
-        v.y = keep_valid(v.y, 2, valid);
-        v.z = keep_valid(v.z, 4, valid);
-        v.w = keep_valid(v.w, 6, valid);
-    }
-    return v;
-}
-__device__ __forceinline__ uint2 load4(const __nv_bfloat16 *at, int valid) {
-    if (valid <= 0) return make_uint2(0, 0);
-    uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
-    if (valid < 4) {
-        v.x = keep_valid(v.x, 0, valid);
-        v.y = keep_valid(v.y, 2, valid);
-    }
-    return v;
+__device__ __forceinline__ void keep8(uint4 &v, int valid) {
+    v.x = keep_valid(v.x, 0, valid);
+    v.y = keep_valid(v.y, 2, valid);
+    v.z = keep_valid(v.z, 4, valid);
+    v.w = keep_valid(v.w, 6, valid);
 }
 __device__ __forceinline__ float remote_f32(unsigned local, unsigned cta) {
     unsigned at;
     float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(cta));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
     return v;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+    unsigned n;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    return n;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -174,7 +244,7 @@ template <int R, bool F32>
 struct Few {
     static constexpr int TERMS = F32 ? 3 : 2;
     static constexpr int T_LD = R + 8;                      // elements of a row of T: the eight rows of a load fall into different banks
-    float red[FEW_THREADS / 32][16][R];
+    float red[FEW_THREADS / 64][16][R];
     float part[16][R];
     __nv_bfloat16 T[TERMS][16][T_LD];
 };
@@ -185,71 +255,165 @@ struct Few {
 // permuted alike in both operands.  Second product: 32 columns of Y at a time, MMA i multiplying with rows
 // 8(g / 2) + 2i + g % 2 of B, which leaves lane (g, t) with eight consecutive columns of rows g and g + 8.
 template <int R, bool F32>
-__global__ void __launch_bounds__(FEW_THREADS)
+__global__ void __maxnreg__(R <= 64 ? 112 : 232)
 mwu_adapters_few_kernel(const Params p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ Finder f;
+    __shared__ union { Finder f; Sorter o; } find;
+    Finder &f = find.f;
     Few<R, F32> *sm = reinterpret_cast<Few<R, F32> *>(smem_raw);
     constexpr int TERMS = Few<R, F32>::TERMS;
     // Beside the tile kernel: that one has waited for what came before it, so the inputs are there; its own rows are others than these.
     if (!p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int c = (int)cluster_rank(), clusters = (int)gridDim.x / FEW_CTAS;
+    const int c = (int)cluster_rank(), ctas = (int)cluster_size(), clusters = (int)gridDim.x / ctas;
     const int per = (p.segments + FEW_THREADS - 1) / FEW_THREADS;
-    int first;
-    const int total = count_items<true, FEW_THREADS>(p, &f, per, first);
+    const bool sorted = p.few_rows != FEW_ROWS;
+    int first = 0;
+    const int total = sorted ? sort_rows(p, &find.o, per) : count_items<true, FEW_THREADS>(p, &f, per, first);
     if (total < 0 && blockIdx.x == 0 && tid == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_BOUNDS);
     const int k_chunks = (p.cols + 31) / 32, n_groups = (p.rows + 31) / 32;
-    const int kc0 = (int)((long long)k_chunks * c / FEW_CTAS), kc1 = (int)((long long)k_chunks * (c + 1) / FEW_CTAS);
-    const int ng0 = (int)((long long)n_groups * c / FEW_CTAS), ng1 = (int)((long long)n_groups * (c + 1) / FEW_CTAS);
+    const int kc0 = (int)((long long)k_chunks * c / ctas), kc1 = (int)((long long)k_chunks * (c + 1) / ctas);
+    const int ng0 = (int)((long long)n_groups * c / ctas), ng1 = (int)((long long)n_groups * (c + 1) / ctas);
 
-    for (int item = (int)blockIdx.x / FEW_CTAS; item < total; item += clusters) {
-        __syncthreads();
-        find_item<true>(p, &f, per, first, item);
-        __syncthreads();
-        const int row0 = f.row0, count = f.count, a = f.adapter;
+    for (int item = (int)blockIdx.x / ctas; item < total; item += clusters) {
+        int row0 = 0, count, a;
+        const int *rows = nullptr;
+        if (sorted) {
+            const int at = find.o.start[item];
+            count = find.o.start[item + 1] - at;
+            rows = &find.o.row[at];
+            a = find.o.key[rows[0]];
+        } else {
+            __syncthreads();
+            find_item<true>(p, &f, per, first, item);
+            __syncthreads();
+            row0 = f.row0;
+            count = f.count;
+            a = f.adapter;
+        }
+        auto row_of = [&](int r) { return rows ? rows[r] : row0 + r; };
         if (a < 0) {
-            copy_rows<F32>(p, row0, count, ng0 * 32, min(p.rows, ng1 * 32), tid, FEW_THREADS);
+            copy_rows<F32, 1>(p, row_of, count, ng0 * 32, min(p.rows, ng1 * 32), tid, FEW_THREADS);
             continue;
         }
+        // this lane's two rows (the first one again where there are fewer: read, never written)
+        const long long r0 = row_of(g < count ? g : 0), r1 = row_of(g + 8 < count ? g + 8 : 0);
         // ---- T = X . A^T over this CTA's slice of cols ----
         float acc[R / 8][4];
 #pragma unroll
         for (int i = 0; i < R / 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-        const __nv_bfloat16 *x0 = p.X + (long long)(row0 + g) * p.ldx + 8 * t, *x1 = x0 + 8 * p.ldx;
+        const __nv_bfloat16 *x0 = p.X + r0 * p.ldx + 8 * t, *x1 = p.X + r1 * p.ldx + 8 * t;
         const __nv_bfloat16 *a0 = p.A + (long long)a * p.a_stride + (long long)g * p.lda + 8 * t;
-        for (int ch = kc0 + warp; ch < kc1; ch += FEW_THREADS / 32) {
-            const int k = ch * 32, valid = p.cols - k - 8 * t;
-            const uint4 u = load8(x0 + k, g < count ? valid : 0), v = load8(x1 + k, g + 8 < count ? valid : 0);
+        constexpr int BATCH = R / 8 < 8 ? R / 8 : 8;        // loads of A in flight, of each of
+        constexpr int AHEAD = R <= 32 ? 2 : 1;              // so many chunks
+        for (int ch = kc0 + warp; ch < kc1; ch += AHEAD * (FEW_THREADS / 32)) {
+            uint4 u[AHEAD], v[AHEAD], w[AHEAD][BATCH];
 #pragma unroll
-            for (int i = 0; i < R / 8; ++i) {
-                const uint4 w = load8(a0 + (long long)(8 * i) * p.lda + k, 8 * i + g < p.rank ? valid : 0);
-                mma_16816(acc[i], u.x, v.x, u.y, v.y, w.x, w.y);
-                mma_16816(acc[i], u.z, v.z, u.w, v.w, w.z, w.w);
+            for (int i0 = 0; i0 < R / 8; i0 += BATCH) {
+#pragma unroll
+                for (int h = 0; h < AHEAD; ++h) {
+                    const int cc = ch + h * (FEW_THREADS / 32), k = cc * 32, valid = cc < kc1 ? p.cols - k - 8 * t : 0;
+                    if (i0 == 0) {
+                        u[h] = load8_if(x0 + k, g < count && valid > 0);
+                        v[h] = load8_if(x1 + k, g + 8 < count && valid > 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i)
+                        w[h][i] = load8_if(a0 + (long long)(8 * (i0 + i)) * p.lda + k, 8 * (i0 + i) + g < p.rank && valid > 0);
+                }
+#pragma unroll
+                for (int h = 0; h < AHEAD; ++h) {
+                    const int k = (ch + h * (FEW_THREADS / 32)) * 32, valid = p.cols - k - 8 * t;
+                    if (p.cols - k < 32) {
+                        keep8(u[h], valid);
+                        keep8(v[h], valid);
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i) keep8(w[h][i], valid);
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        mma_16816(acc[i0 + i], u[h].x, v[h].x, u[h].y, v[h].y, w[h][i].x, w[h][i].y);
+                        mma_16816(acc[i0 + i], u[h].z, v[h].z, u[h].w, v[h].w, w[h][i].z, w[h][i].w);
+                    }
+                }
             }
         }
+        // the warps' sums, the upper four onto the lower four first (half the memory: a CTA fits beside one of the tile kernel)
+        float2 *mine = reinterpret_cast<float2 *>(&sm->red[warp % (FEW_THREADS / 64)][g][2 * t]);
 #pragma unroll
-        for (int i = 0; i < R / 8; ++i) {
-            *reinterpret_cast<float2 *>(&sm->red[warp][g][8 * i + 2 * t]) = make_float2(acc[i][0], acc[i][1]);
-            *reinterpret_cast<float2 *>(&sm->red[warp][g + 8][8 * i + 2 * t]) = make_float2(acc[i][2], acc[i][3]);
+        for (int up = 1; up >= 0; --up) {
+            if (warp / (FEW_THREADS / 64) == up) {
+#pragma unroll
+                for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float2 *at = mine + h * 4 * R + 4 * i;          // eight rows on, eight ranks on
+                        float2 v = make_float2(acc[i][2 * h], acc[i][2 * h + 1]);
+                        if (up == 0) {
+                            const float2 o = *at;
+                            v.x += o.x;
+                            v.y += o.y;
+                        }
+                        *at = v;
+                    }
+            }
+            __syncthreads();
         }
-        __syncthreads();
         for (int e = tid; e < 16 * R; e += FEW_THREADS) {
             float s = 0.f;
 #pragma unroll
-            for (int w = 0; w < FEW_THREADS / 32; ++w) s += (&sm->red[w][0][0])[e];
+            for (int w = 0; w < FEW_THREADS / 64; ++w) s += (&sm->red[w][0][0])[e];
             (&sm->part[0][0])[e] = s;
         }
         cluster_arrive();
+        // the operands of this warp's first columns travel meanwhile
+        const __nv_bfloat16 *b0 = p.B + (long long)a * p.b_stride + (R >= 32 ? 8 : 4) * t;
+        constexpr int WIDE = R >= 32 ? 32 : 16;             // ranks of a load of the warp: 16 or 8 bytes a lane
+        constexpr int AT_ONCE = R <= 32 ? 2 : 1;            // runs of 32 columns a warp has under way
+        constexpr int STEP = AT_ONCE * (FEW_THREADS / 32);
+        uint4 w[AT_ONCE][4][R / WIDE];
+        uint4 y0[AT_ONCE][2][F32 ? 2 : 1];
+        auto load_groups = [&](int grp0) {
+#pragma unroll
+            for (int z = 0; z < AT_ONCE; ++z) {
+                const int grp = grp0 + z * (FEW_THREADS / 32);
+                const bool here = grp < ng1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = grp * 32 + 8 * (g >> 1) + 2 * i + (g & 1);
+#pragma unroll
+                    for (int s = 0; s < R / WIDE; ++s) {
+                        const __nv_bfloat16 *at = b0 + (long long)n * p.ldb + WIDE * s;
+                        if constexpr (R >= 32) {
+                            w[z][i][s] = load8_if(at, here && n < p.rows && 32 * s + 8 * t < p.rank);
+                        } else {
+                            const uint2 v = load4_if(at, here && n < p.rows && 4 * t < p.rank);
+                            w[z][i][s] = make_uint4(v.x, v.y, 0, 0);
+                        }
+                    }
+                }
+                const int n = grp * 32 + 8 * t;
+                const unsigned char *from = reinterpret_cast<const unsigned char *>(p.Y0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < (F32 ? 2 : 1); ++e) {
+                        y0[z][h][e] = make_uint4(0, 0, 0, 0);
+                        if (p.Y0 && here && g + 8 * h < count && n + 8 <= p.rows)
+                            y0[z][h][e] = *reinterpret_cast<const uint4 *>(from + ((h ? r1 : r0) * p.ldy + n) * (F32 ? 4 : 2) + 16 * e);
+                    }
+            }
+        };
+        load_groups(ng0 + warp);
         cluster_wait();
         // ---- the cluster's sum, scaled, as bf16 terms ----
         const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
         for (int e = tid; e < 16 * R; e += FEW_THREADS) {
             float s = 0.f;
-#pragma unroll
-            for (int o = 0; o < FEW_CTAS; ++o) s += remote_f32(smem_u32(&(&sm->part[0][0])[e]), (unsigned)o);
+#pragma unroll 4
+            for (int o = 0; o < ctas; ++o) s += remote_f32(smem_u32(&(&sm->part[0][0])[e]), (unsigned)o);
             s *= scale;
 #pragma unroll
             for (int q = 0; q < TERMS; ++q) {
@@ -261,69 +425,89 @@ mwu_adapters_few_kernel(const Params p) {
         cluster_arrive();                                   // the others' sums have been read; waited for below
         __syncthreads();
         // ---- Y = Y0 + T . B^T over this CTA's slice of rows ----
-        const __nv_bfloat16 *b0 = p.B + (long long)a * p.b_stride + 4 * t;
-        for (int grp = ng0 + warp; grp < ng1; grp += FEW_THREADS / 32) {
-            const int n0 = grp * 32;
-            float d[4][4];
-            uint2 w[4][R / 16];
+        for (int grp0 = ng0 + warp; grp0 < ng1; grp0 += STEP) {
+          float d[AT_ONCE][4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
+          for (int z = 0; z < AT_ONCE; ++z) {
 #pragma unroll
-                for (int s = 0; s < R / 16; ++s) w[i][s] = load4(b0 + (long long)n * p.ldb + 16 * s, n < p.rows ? p.rank - 16 * s - 4 * t : 0);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d[i][j] = 0.f;
+                for (int j = 0; j < 4; ++j) d[z][i][j] = 0.f;
+            if (p.rank & (R >= 32 ? 7 : 3)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int s = 0; s < R / WIDE; ++s) keep8(w[z][i][s], p.rank - WIDE * s - (R >= 32 ? 8 : 4) * t);
+            }
+          }
+#pragma unroll
+          for (int s = 0; s < R / WIDE; ++s)
+#pragma unroll
+            for (int q = TERMS - 1; q >= 0; --q) {
+                if constexpr (R >= 32) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(&sm->T[q][g][32 * s + 8 * t]);
+                    const uint4 v = *reinterpret_cast<const uint4 *>(&sm->T[q][g + 8][32 * s + 8 * t]);
+#pragma unroll
+                    for (int z = 0; z < AT_ONCE; ++z)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            mma_16816(d[z][i], u.x, v.x, u.y, v.y, w[z][i][s].x, w[z][i][s].y);
+                            mma_16816(d[z][i], u.z, v.z, u.w, v.w, w[z][i][s].z, w[z][i][s].w);
+                        }
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(&sm->T[q][g][4 * t]);
+                    const uint2 v = *reinterpret_cast<const uint2 *>(&sm->T[q][g + 8][4 * t]);
+#pragma unroll
+                    for (int z = 0; z < AT_ONCE; ++z)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_16816(d[z][i], u.x, v.x, u.y, v.y, w[z][i][s].x, w[z][i][s].y);
+                }
             }
 #pragma unroll
-            for (int s = 0; s < R / 16; ++s)
-#pragma unroll
-                for (int q = TERMS - 1; q >= 0; --q) {
-                    const uint2 u = *reinterpret_cast<const uint2 *>(&sm->T[q][g][16 * s + 4 * t]);
-                    const uint2 v = *reinterpret_cast<const uint2 *>(&sm->T[q][g + 8][16 * s + 4 * t]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mma_16816(d[i], u.x, v.x, u.y, v.y, w[i][s].x, w[i][s].y);
-                }
-            const int n = n0 + 8 * t, left = p.rows - n;
+          for (int z = 0; z < AT_ONCE; ++z) {
+            const int grp = grp0 + z * (FEW_THREADS / 32);
+            if (grp >= ng1) break;
+            const int n = grp * 32 + 8 * t, left = p.rows - n;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (g + 8 * h >= count || left <= 0) continue;
-                const long long at = (long long)(row0 + g + 8 * h) * p.ldy + n;
+                const long long at = (h ? r1 : r0) * p.ldy + n;
+                const unsigned in[8] = {y0[z][h][0].x, y0[z][h][0].y, y0[z][h][0].z, y0[z][h][0].w, y0[z][h][F32].x, y0[z][h][F32].y, y0[z][h][F32].z, y0[z][h][F32].w};
                 if (F32) {
                     float *y = reinterpret_cast<float *>(p.Y) + at;
-                    const float *y0 = reinterpret_cast<const float *>(p.Y0) + at;
+                    if (left >= 8) {
+                        float o[8];
 #pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        if (left >= 2 * i + 4) {
-                            float4 b = p.Y0 ? *reinterpret_cast<const float4 *>(y0 + 2 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
-                            b.x += d[i][2 * h]; b.y += d[i][2 * h + 1]; b.z += d[i + 1][2 * h]; b.w += d[i + 1][2 * h + 1];
-                            *reinterpret_cast<float4 *>(y + 2 * i) = b;
-                        } else {
+                        for (int j = 0; j < 8; ++j) o[j] = __uint_as_float(in[j]) + d[z][j / 2][2 * h + j % 2];
+                        *reinterpret_cast<float4 *>(y) = make_float4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<float4 *>(y + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                    } else {
+                        const float *b = reinterpret_cast<const float *>(p.Y0) + at;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (2 * i + j < left) y[2 * i + j] = (p.Y0 ? y0[2 * i + j] : 0.f) + d[i + j / 2][2 * h + j % 2];
-                        }
+                        for (int j = 0; j < 8; ++j)
+                            if (j < left) y[j] = (p.Y0 ? b[j] : 0.f) + d[z][j / 2][2 * h + j % 2];
                     }
                 } else {
                     __nv_bfloat16 *y = reinterpret_cast<__nv_bfloat16 *>(p.Y) + at;
-                    const __nv_bfloat16 *y0 = reinterpret_cast<const __nv_bfloat16 *>(p.Y0) + at;
                     if (left >= 8) {
-                        const uint4 b = p.Y0 ? *reinterpret_cast<const uint4 *>(y0) : make_uint4(0, 0, 0, 0);
-                        const unsigned in[4] = {b.x, b.y, b.z, b.w};
                         unsigned out[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const __nv_bfloat162 o = __floats2bfloat162_rn(__uint_as_float(in[i] << 16) + d[i][2 * h],
-                                                                           __uint_as_float(in[i] & 0xffff0000u) + d[i][2 * h + 1]);
+                            const __nv_bfloat162 o = __floats2bfloat162_rn(__uint_as_float(in[i] << 16) + d[z][i][2 * h],
+                                                                           __uint_as_float(in[i] & 0xffff0000u) + d[z][i][2 * h + 1]);
                             out[i] = *reinterpret_cast<const unsigned *>(&o);
                         }
                         *reinterpret_cast<uint4 *>(y) = make_uint4(out[0], out[1], out[2], out[3]);
                     } else {
+                        const __nv_bfloat16 *b = reinterpret_cast<const __nv_bfloat16 *>(p.Y0) + at;
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            if (j < left) y[j] = __float2bfloat16_rn((p.Y0 ? __bfloat162float(y0[j]) : 0.f) + d[j / 2][2 * h + j % 2]);
+                            if (j < left) y[j] = __float2bfloat16_rn((p.Y0 ? __bfloat162float(b[j]) : 0.f) + d[z][j / 2][2 * h + j % 2]);
                     }
                 }
             }
+          }
+          load_groups(grp0 + STEP);
         }
         cluster_wait();
     }
@@ -334,34 +518,39 @@ mwu_adapters_few_kernel(const Params p) {
 // many rows
 // ------------------------------------------------------------------------------------------
 // A stage of the first product: 128 rows x 64 columns of X and R x 64 of A.  A chunk of the second: 128 rows x 128 bytes of Y0
-// (64 columns of bf16, 32 of fp32) and as many rows of B.  Two rings, so that the first chunks of Y0 and B come in while T is still being added up.
+// (64 columns of bf16, 32 of fp32) and as many rows of B.  Both go through the same ring of slots, so the first chunks of Y0 and B come
+// in while T is still being added up.
+// This kernel's clusters hold tensor memory while their CTAs wait for one another.  Were a CTA of another such kernel (on another
+// stream) on the same SM, each could hold what the other waits for; with this much shared memory none fits beside it (the least
+// that such a kernel takes is 36 KB), but a CTA of the kernel for few rows does.
+constexpr int TILE_SMEM = 196 * 1024;
+
 template <int R, bool F32>
 struct TileCfg {
     static constexpr int TERMS = F32 ? 3 : 2;
     static constexpr int CW = F32 ? 32 : 64;                // columns of Y in a chunk
     static constexpr int BLOCKS = R > 64 ? 2 : 1;           // 64 ranks to a 128-byte row
     static constexpr int ROWS_BYTES = 128 * 128;
-    static constexpr int IN_SLOT = ROWS_BYTES + (R < 64 ? 8192 : R * 128);
-    static constexpr int OUT_SLOT = ROWS_BYTES + (F32 ? 4096 : 8192) * BLOCKS;
+    static constexpr int SLOT = ROWS_BYTES + 8192 * BLOCKS;
     static constexpr int T_BYTES = TERMS * BLOCKS * ROWS_BYTES;
-    static constexpr int IN_SLOTS = R > 64 ? (F32 ? 2 : 3) : 4;
-    static constexpr int OUT_SLOTS = R > 64 ? 2 : 3;
-    static constexpr int SMEM = T_BYTES + IN_SLOTS * IN_SLOT + OUT_SLOTS * OUT_SLOT;
-    static_assert(IN_SLOTS * IN_SLOT >= 128 * R * 4, "the ring of the first product takes its sums afterwards");
+    static constexpr bool POW2 = R > 64 && F32;             // only clusters of 1, 2, 4 or 8 fit
+    static constexpr int SUM_BYTES = (POW2 ? 128 : 133) * R * 4;    // of at most 8 CTAs' shares of 128 rows, each rounded up
+    static constexpr int EXTRA = 1024 + 1024;               // alignment, and what TileSmem takes
+    static constexpr int MOST = R > 64 ? 227 * 1024 : TILE_SMEM;
+    static constexpr int FIT = (MOST - EXTRA - T_BYTES - SUM_BYTES) / SLOT;
+    static constexpr int SLOTS = FIT < 6 ? FIT : 6;
+    static constexpr int USED = EXTRA + T_BYTES + SUM_BYTES + SLOTS * SLOT;
+    static constexpr int SMEM = USED < TILE_SMEM ? TILE_SMEM : USED;
+    static_assert(SLOTS >= 2 && SMEM <= 227 * 1024 && 64 * 128 >= CW * 128, "adapter tile kernel: shared memory");
 };
 
 struct TileSmem {
-    unsigned long long full1[4], empty1[4], full2[3], empty2[3], tfull1[2], tempty1[2], tfull2[2], tempty2[2], drain;
+    unsigned long long full[6], empty1[6], empty2[6], tfull1[2], tempty1[2], tfull2[2], tempty2[2], drain;
     unsigned tmem_base;
     int abort, drain_abort;
     Finder f;
 };
-
-template <int R, bool F32>
-constexpr int tile_smem() { return 1024 + TileCfg<R, F32>::SMEM + (int)sizeof(TileSmem); }
-// This kernel's clusters hold tensor memory while their CTAs wait for one another.  Were a CTA of another such kernel (on another
-// stream) on the same SM, each could hold what the other waits for; with this much shared memory none fits beside it.
-constexpr int TILE_LEAST_SMEM = 196 * 1024;
+static_assert(sizeof(TileSmem) <= 1024, "adapter tile kernel: shared memory");
 
 __device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int y, int z) {
     asm volatile(
@@ -378,11 +567,6 @@ __device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned (&r)[16]) {
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
-__device__ __forceinline__ unsigned cluster_size() {
-    unsigned n;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
-    return n;
-}
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
 template <int R, bool F32>
@@ -393,20 +577,18 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
     using C = TileCfg<R, F32>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *sT = smem_raw + smem_pad_1024(smem_raw);
-    unsigned char *s1 = sT + C::T_BYTES, *s2 = s1 + C::IN_SLOTS * C::IN_SLOT;
-    TileSmem *sm = reinterpret_cast<TileSmem *>(s2 + C::OUT_SLOTS * C::OUT_SLOT);
+    unsigned char *ring = sT + C::T_BYTES;
+    float4 *sums = reinterpret_cast<float4 *>(ring + C::SLOTS * C::SLOT);
+    TileSmem *sm = reinterpret_cast<TileSmem *>(reinterpret_cast<unsigned char *>(sums) + C::SUM_BYTES);
     volatile int *abort = &sm->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ctas = (int)cluster_size(), c = (int)cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::IN_SLOTS; ++s) {
-            mbar_init(smem_u32(&sm->full1[s]), 1);
-            mbar_init(smem_u32(&sm->empty1[s]), 1);
-        }
-        for (int s = 0; s < C::OUT_SLOTS; ++s) {
-            mbar_init(smem_u32(&sm->full2[s]), 1);
-            mbar_init(smem_u32(&sm->empty2[s]), 4);
+        for (int s = 0; s < C::SLOTS; ++s) {
+            mbar_init(smem_u32(&sm->full[s]), 1);
+            mbar_init(smem_u32(&sm->empty1[s]), 1);         // released by the first product's MMAs
+            mbar_init(smem_u32(&sm->empty2[s]), 4);         // ... by four warps of the epilogue
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sm->tfull1[b]), 1);
@@ -432,6 +614,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
     if (item < total) find_item<false>(p, &sm->f, per, first, item);
     tc_fence_before();
     __syncthreads();
+    cluster_arrive();                                       // the others may write into this CTA's memory; waited for before the first write
     tc_fence_after();
     const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
     const bool work = item < total;                         // the whole cluster alike
@@ -443,37 +626,40 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
     constexpr int PIECE = 8;                                // stages between two sums of T (512 products)
 
     if (work && a < 0) {
-        copy_rows<F32>(p, row0, count, nc0 * C::CW, min(p.rows, nc1 * C::CW), threadIdx.x, TILE_THREADS);
+        copy_rows<F32, 8>(p, [&](int r) { return row0 + r; }, count, nc0 * C::CW, min(p.rows, nc1 * C::CW), threadIdx.x, TILE_THREADS);
     } else if (work && warp == 0) {
         // ---------------- TMA producer ----------------
         bool ok = true;
-        int n1 = 0, n2 = 0;                                 // stages and chunks asked for so far
-        for (int ks = ks0; ks < ks1; ++ks, ++n1) {
-            const int s = n1 % C::IN_SLOTS;
-            ok = warp_wait_spin(smem_u32(&sm->empty1[s]), ((unsigned)(n1 / C::IN_SLOTS) & 1u) ^ 1u, abort);
+        const int n1 = ks1 - ks0, n2 = nc1 - nc0;           // stages and chunks
+        int n = 0;                                          // slots filled so far
+        for (; n < n1; ++n) {
+            const int s = n % C::SLOTS, ks = ks0 + n;
+            if (n >= C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty1[s]), (unsigned)(n / C::SLOTS - 1) & 1u, abort);
             if (!ok) break;
             if (elect_one()) {
-                const unsigned bar = smem_u32(&sm->full1[s]), dst = smem_u32(s1 + s * C::IN_SLOT);
+                const unsigned bar = smem_u32(&sm->full[s]), dst = smem_u32(ring + s * C::SLOT);
                 mbar_expect_tx(bar, (unsigned)(bands * 4096 + R * 128));
                 for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_x, bar, ks * 64, row0 + 32 * b);
                 tma_load_3d(dst + C::ROWS_BYTES, &tm_a, bar, ks * 64, 0, a);
             }
             __syncwarp();
         }
+        cluster_wait();
         cluster_arrive();
         bool waited = false;
-        for (int i = nc0; i < nc1 && ok; ++i, ++n2) {
-            const int s = n2 % C::OUT_SLOTS;
-            if (n2 == C::OUT_SLOTS) {                       // the first slots are free; the others need T
+        for (; n < n1 + n2 && ok; ++n) {
+            const int s = n % C::SLOTS, i = nc0 + n - n1;
+            if (n == n1 + C::SLOTS) {                       // slots of the first product are used up; the others need T
                 cluster_wait();
                 cluster_arrive();
                 cluster_wait();
                 waited = true;
             }
-            ok = warp_wait_spin(smem_u32(&sm->empty2[s]), ((unsigned)(n2 / C::OUT_SLOTS) & 1u) ^ 1u, abort);
+            if (n >= n1 + C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty2[s]), (unsigned)((n - n1) / C::SLOTS - 1) & 1u, abort);
+            else if (n >= C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty1[s]), (unsigned)(n / C::SLOTS - 1) & 1u, abort);
             if (!ok) break;
             if (elect_one()) {
-                const unsigned bar = smem_u32(&sm->full2[s]), dst = smem_u32(s2 + s * C::OUT_SLOT);
+                const unsigned bar = smem_u32(&sm->full[s]), dst = smem_u32(ring + s * C::SLOT);
                 mbar_expect_tx(bar, (unsigned)((p.Y0 ? bands * 4096 : 0) + C::CW * 128 * C::BLOCKS));
                 for (int q = 0; q < C::BLOCKS; ++q)
                     tma_load_3d(dst + C::ROWS_BYTES + q * C::CW * 128, &tm_b, bar, 64 * q, i * C::CW, a);
@@ -489,10 +675,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
         }
         // a wait ran out: the loads in flight land before this CTA leaves
         if (__any_sync(0xffffffffu, *abort)) {
-            for (int s = 0; s < C::IN_SLOTS; ++s)
-                if (n1 > s) mbar_wait(smem_u32(&sm->full1[s]), (unsigned)((n1 - s - 1) / C::IN_SLOTS) & 1u, &sm->drain_abort);
-            for (int s = 0; s < C::OUT_SLOTS; ++s)
-                if (n2 > s) mbar_wait(smem_u32(&sm->full2[s]), (unsigned)((n2 - s - 1) / C::OUT_SLOTS) & 1u, &sm->drain_abort);
+            for (int s = 0; s < C::SLOTS; ++s)
+                if (n > s) mbar_wait(smem_u32(&sm->full[s]), (unsigned)((n - s - 1) / C::SLOTS) & 1u, &sm->drain_abort);
             __syncwarp();
         }
     } else if (work && warp == 1) {
@@ -506,13 +690,13 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             tc_fence_after();
             const int k1 = min(ks1, k0 + PIECE);
             for (int ks = k0; ks < k1; ++ks, ++n) {
-                const int s = n % C::IN_SLOTS;
-                ok = warp_wait_spin(smem_u32(&sm->full1[s]), (unsigned)(n / C::IN_SLOTS) & 1u, abort);
+                const int s = n % C::SLOTS;
+                ok = warp_wait_spin(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const unsigned long long xd = make_desc(smem_u32(s1 + s * C::IN_SLOT));
-                    const unsigned long long ad = make_desc(smem_u32(s1 + s * C::IN_SLOT + C::ROWS_BYTES));
+                    const unsigned long long xd = make_desc(smem_u32(ring + s * C::SLOT));
+                    const unsigned long long ad = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES));
 #pragma unroll
                     for (int k4 = 0; k4 < 4; ++k4)
                         umma_bf16(tmem_base + (use & 1u) * R, xd + 2ull * k4, ad + 2ull * k4, make_idesc(R), (ks > k0 || k4) ? 1u : 0u);
@@ -524,17 +708,18 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             if (elect_one()) umma_commit(smem_u32(&sm->tfull1[use & 1u]));
             __syncwarp();
         }
+        cluster_wait();
         cluster_arrive();
         cluster_wait();
         cluster_arrive();
         cluster_wait();                                     // T of all rows is here, as bf16 terms
         fence_proxy_async_all();
-        n = 0;
-        for (int i = nc0; ok && i < nc1; ++i, ++n) {
-            const int s = n % C::OUT_SLOTS;
-            const unsigned buf = (unsigned)n & 1u;
-            ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((unsigned)(n >> 1) & 1u) ^ 1u, abort) &&
-                 warp_wait_spin(smem_u32(&sm->full2[s]), (unsigned)(n / C::OUT_SLOTS) & 1u, abort);
+        n = ks1 - ks0;
+        for (int j = 0; ok && j < nc1 - nc0; ++j, ++n) {
+            const int s = n % C::SLOTS;
+            const unsigned buf = (unsigned)j & 1u;
+            ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((unsigned)(j >> 1) & 1u) ^ 1u, abort) &&
+                 warp_wait_spin(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -542,10 +727,10 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
 #pragma unroll
                 for (int q = C::TERMS - 1; q >= 0; --q)     // the smallest term first
 #pragma unroll
-                    for (int j = 0; j < R / 16; ++j) {
-                        const unsigned long long td = make_desc(smem_u32(sT + (q * C::BLOCKS + j / 4) * C::ROWS_BYTES));
-                        const unsigned long long bd = make_desc(smem_u32(s2 + s * C::OUT_SLOT + C::ROWS_BYTES + (j / 4) * C::CW * 128));
-                        umma_bf16(tmem_base + 256u + buf * 64u, td + 2ull * (j % 4), bd + 2ull * (j % 4), make_idesc(C::CW), acc);
+                    for (int r = 0; r < R / 16; ++r) {
+                        const unsigned long long td = make_desc(smem_u32(sT + (q * C::BLOCKS + r / 4) * C::ROWS_BYTES));
+                        const unsigned long long bd = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES + (r / 4) * C::CW * 128));
+                        umma_bf16(tmem_base + 256u + buf * 64u, td + 2ull * (r % 4), bd + 2ull * (r % 4), make_idesc(C::CW), acc);
                         acc = 1;
                     }
                 umma_commit(smem_u32(&sm->tfull2[buf]));
@@ -587,36 +772,41 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm->tempty1[use & 1u]));
         }
-        // four ranks of a row to 16 bytes, rows next to one another.  (The first product's ring is free: its last MMA has been waited for.)
-        float4 *part = reinterpret_cast<float4 *>(s1);
+        // To the CTA that adds up this row: [CTA it comes from][four ranks][row], 16 bytes each, rows next to one another.
+        const int owner = ((row + 1) * ctas - 1) / 128, most = (128 + ctas - 1) / ctas;
+        const unsigned there = smem_u32(sums + (c * (R / 4) + col0 / 4) * most + row - 128 * owner / ctas);
+        cluster_wait();                                     // all CTAs are there
         if (R >= 64 || half == 0) {
+            unsigned at;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(there), "r"(owner));
 #pragma unroll
             for (int j = 0; j < MINE / 4; ++j)
-                part[(col0 / 4 + j) * 128 + row] = make_float4(t[4 * j], t[4 * j + 1], t[4 * j + 2], t[4 * j + 3]);
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                             ::"r"(at + (unsigned)(j * most * 16)), "f"(t[4 * j]), "f"(t[4 * j + 1]), "f"(t[4 * j + 2]), "f"(t[4 * j + 3]) : "memory");
         }
         cluster_arrive();
         cluster_wait();
         // ---------------- this CTA's share of the rows: added up, scaled, split, given to all ----------------
         const int r0 = 128 * c / ctas, nr = 128 * (c + 1) / ctas - r0;
         const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
-        for (int e = tid; e < nr * (R / 4); e += 256) {
-            const int r = r0 + e % nr, q4 = e / nr;
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int o = 0; o < ctas; ++o) {
-                unsigned at;
-                float4 v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(part + q4 * 128 + r)), "r"(o));
-                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        for (int e = tid; e < nr * (R / 8); e += 256) {
+            const int rr = e % nr, q8 = e / nr, r = r0 + rr;
+            float f[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int o = 0; o < ctas; ++o) {
+                    const float4 v = sums[(o * (R / 4) + 2 * q8 + h) * most + rr];
+                    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+                }
+                f[4 * h] = s.x * scale; f[4 * h + 1] = s.y * scale; f[4 * h + 2] = s.z * scale; f[4 * h + 3] = s.w * scale;
             }
-            float f[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
-            const unsigned place = (unsigned)(q4 / 16) * C::ROWS_BYTES + (r >> 3) * 1024u + (r & 7) * 128u +
-                                   ((((unsigned)q4 >> 1 & 7u) ^ (r & 7)) << 4) + (q4 & 1) * 8u;
+            const unsigned place = smem_u32(sT) + (unsigned)(q8 / 8) * C::ROWS_BYTES + swz((unsigned)r, (unsigned)q8 & 7u);
 #pragma unroll
             for (int q = 0; q < C::TERMS; ++q) {
-                unsigned w[2];
+                unsigned w[4];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < 4; ++j) {
                     const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
                     w[j] = *reinterpret_cast<const unsigned *>(&h);
                     f[2 * j] -= __low2float(h);
@@ -624,9 +814,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                 }
                 for (int o = 0; o < ctas; ++o) {
                     unsigned at;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                                 : "=r"(at) : "r"(smem_u32(sT) + (unsigned)(q * C::BLOCKS * C::ROWS_BYTES) + place), "r"(o));
-                    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w[0]), "r"(w[1]) : "memory");
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(place + (unsigned)(q * C::BLOCKS * C::ROWS_BYTES)), "r"(o));
+                    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                 }
             }
         }
@@ -635,10 +824,10 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
         cluster_wait();
         // ---------------- chunks of Y: four warps take the even ones, four the odd ones ----------------
         const int rows_here = min(32, max(0, count - quarter * 32));
-        for (int i = nc0 + half, n = half; ok && i < nc1; i += 2, n += 2) {
-            const int s = n % C::OUT_SLOTS;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), (unsigned)(n >> 1) & 1u, abort) &&
-                                             mbar_wait(smem_u32(&sm->full2[s]), (unsigned)(n / C::OUT_SLOTS) & 1u, abort));
+        for (int j = half; ok && j < nc1 - nc0; j += 2) {
+            const int i = nc0 + j, n = ks1 - ks0 + j, s = n % C::SLOTS;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), (unsigned)(j >> 1) & 1u, abort) &&
+                                             mbar_wait(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort));
             if (!ok) break;
             tc_fence_after();
             unsigned v[C::CW / 32][32];
@@ -648,7 +837,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm->tempty2[half]));
-            unsigned char *box = s2 + s * C::OUT_SLOT + quarter * 4096;
+            unsigned char *box = ring + s * C::SLOT + quarter * 4096;
             const int n0 = i * C::CW;
             if (rows_here > 0) {
 #pragma unroll
@@ -712,6 +901,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
         __syncwarp();
     }
 
+    if (!work || a < 0) cluster_wait();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -733,13 +923,17 @@ static cudaError_t launch_few(const Params &p, int sm_count, cudaStream_t st) {
     const size_t smem = sizeof(Few<R, F32>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    // a cluster for every 16 rows that there may be in such segments, as far as four CTAs an SM go; more items are taken in turn
-    long long items = (long long)p.segments + p.M / 16;
-    if (items > 2ll * p.segments) items = 2ll * p.segments;
+    // a cluster for every 16 rows that there may be of a segment or an adapter, as far as four CTAs an SM go; more items are taken in turn
+    long long items = p.M / 16 + (p.few_rows == FEW_ROWS ? (long long)p.segments : p.adapters + 1ll);
+    if (p.few_rows == FEW_ROWS && items > 2ll * p.segments) items = 2ll * p.segments;
     if (items > p.M) items = p.M;
-    const long long most = 4ll * sm_count / FEW_CTAS;
+    // CTAs to a cluster: as many as leave the SMs with two or three (64 rows of 32 adapters, 4096 -> 16384, rank 32: 16.6 us with eight,
+    // 19.9 with six, 20.4 with four; beside 2777 rows of prompts, 61 rows, 1216 -> 1000: 23.6 with two, 24.4 / 31.1 with four / eight)
+    long long ctas = 5ll * sm_count / (2 * items);
+    ctas = ctas < 2 ? 2 : ctas > 8 ? 8 : ctas;
+    const long long most = 4ll * sm_count / ctas;
     count_launch();
-    return launch_chained(kern, dim3((unsigned)(FEW_CTAS * (items < most ? items : most))), dim3(FEW_THREADS), smem, st, FEW_CTAS, p);
+    return launch_chained(kern, dim3((unsigned)(ctas * (items < most ? items : most))), dim3(FEW_THREADS), smem, st, (int)ctas, p);
 }
 
 static bool encode(CUtensorMap *tm, const void *ptr, bool fp32, int64_t inner, int64_t rows, int64_t ld, int box_rows, int64_t n, int64_t stride) {
@@ -757,8 +951,7 @@ template <int R, bool F32>
 static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
     auto kern = mwu_adapters_tile_kernel<R, F32>;
     using C = TileCfg<R, F32>;
-    constexpr int smem = tile_smem<R, F32>() > TILE_LEAST_SMEM ? tile_smem<R, F32>() : TILE_LEAST_SMEM;
-    static_assert(smem <= 232448, "adapter tile kernel: shared memory above 227 KB");
+    constexpr int smem = C::SMEM;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MWU_ERR_CUDA;
     if (!get_encode_fn()) return MWU_ERR_CUDA;
     CUtensorMap tm_x, tm_a, tm_b, tm_y0, tm_y;
@@ -772,6 +965,7 @@ static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
     const long long most = p.M / 128 + some, expected = (p.M + 127) / 128 + (some < p.M / 256 ? some : p.M / 256);
     long long ctas = sm_count / expected;
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
+    if (C::POW2) ctas = ctas >= 8 ? 8 : ctas >= 4 ? 4 : ctas >= 2 ? 2 : 1;
     count_launch();
     return launch_chained(kern, dim3((unsigned)(most * ctas)), dim3(TILE_THREADS), smem, st, (int)ctas, tm_x, tm_a, tm_b, tm_y0, tm_y, p) ==
                    cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
@@ -779,7 +973,9 @@ static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
 
 template <int R, bool F32>
 static int launch_both(Params p, int sm_count, cudaStream_t st) {
-    if (p.M > FEW_ROWS) {
+    p.few_rows = 0x7fffffff;
+    if (p.M > FEW_IN_ALL) {
+        p.few_rows = FEW_ROWS;
         const int rc = launch_tile<R, F32>(p, sm_count, st);
         if (rc != MWU_OK) return rc;
         p.beside = 1;
