@@ -31,6 +31,7 @@ constexpr int FEW_IN_ALL = 256;         // and rows of a call that it takes what
 constexpr int FEW_THREADS = 256;
 static_assert(FEW_IN_ALL == FEW_THREADS, "a thread sorts one row");
 constexpr int TILE_THREADS = 320;
+constexpr int TILE_ROWS = 128;          // rows of an item of the tile kernel
 
 struct Params {
     const __nv_bfloat16 *A, *B, *X;
@@ -55,7 +56,7 @@ struct Finder {
 
 // rows of a segment that lie in one work item, or 0 where the segment is the other kernel's
 template <bool FEW>
-__device__ __forceinline__ int item_rows(const Params &p, int len) { return (len <= p.few_rows) == FEW ? (FEW ? 16 : 128) : 0; }
+__device__ __forceinline__ int item_rows(const Params &p, int len) { return (len <= p.few_rows) == FEW ? (FEW ? 16 : TILE_ROWS) : 0; }
 
 // Thread i looks after segments i * per .. of the list; its items are number `first` and on.  Returns how many there are in all,
 // -1 where the list makes no sense.  All threads of the CTA.
@@ -163,34 +164,34 @@ __device__ __forceinline__ int sort_rows(const Params &p, Sorter *o, int per) {
     return total;
 }
 
-// Y = Y0 (or zeros) for rows without an adapter, columns n0 .. n1 (n0 a multiple of 32), 16 bytes at a time, AT_ONCE of them in flight
+// Y = Y0 (or zeros) for rows without an adapter, columns n0 .. n1 (n0 a multiple of 32): a row to a warp, 16 bytes to a lane, AT_ONCE of
+// them in flight
 template <bool F32, int AT_ONCE, typename RowOf>
-__device__ __forceinline__ void copy_rows(const Params &p, RowOf row_of, int count, int n0, int n1, int tid, int threads) {
+__device__ __forceinline__ void copy_rows(const Params &p, RowOf row_of, int count, int n0, int n1, int warp, int warps) {
     if (p.Y0 == p.Y || n1 <= n0) return;
     constexpr int SIZE = F32 ? 4 : 2, UNIT = 16 / SIZE;
-    const unsigned char *from = reinterpret_cast<const unsigned char *>(p.Y0);
-    unsigned char *to = reinterpret_cast<unsigned char *>(p.Y);
-    const unsigned units = (unsigned)(n1 - n0 + UNIT - 1) / UNIT;
-    for (unsigned e0 = tid; e0 < units * (unsigned)count; e0 += AT_ONCE * threads) {
-        uint4 v[AT_ONCE];
-        long long at[AT_ONCE];
-        int left[AT_ONCE];
+    const int lane = threadIdx.x & 31, whole = (n1 - n0) / UNIT;
+#pragma unroll 1
+    for (int r = warp; r < count; r += warps) {
+        const long long at = ((long long)row_of(r) * p.ldy + n0) * SIZE;
+        const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(p.Y0) + at);
+        uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.Y) + at);
+#pragma unroll 1
+        for (int u = lane; u < whole; u += 32 * AT_ONCE) {
+            uint4 v[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const unsigned e = e0 + j * threads, r = e / units;
-            const int n = n0 + (int)(e - r * units) * UNIT;
-            left[j] = e < units * (unsigned)count ? n1 - n : 0;
-            if (left[j] <= 0) continue;
-            at[j] = ((long long)row_of((int)r) * p.ldy + n) * SIZE;
-            v[j] = make_uint4(0, 0, 0, 0);
-            if (from && left[j] >= UNIT) v[j] = *reinterpret_cast<const uint4 *>(from + at[j]);
+            for (int j = 0; j < AT_ONCE; ++j) {
+                v[j] = make_uint4(0, 0, 0, 0);
+                if (p.Y0 && u + 32 * j < whole) v[j] = from[u + 32 * j];
+            }
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j)
+                if (u + 32 * j < whole) to[u + 32 * j] = v[j];
         }
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            if (left[j] >= UNIT) *reinterpret_cast<uint4 *>(to + at[j]) = v[j];
-            else
-                for (int b = 0; b < left[j] * SIZE; b += 2)
-                    *reinterpret_cast<unsigned short *>(to + at[j] + b) = from ? *reinterpret_cast<const unsigned short *>(from + at[j] + b) : (unsigned short)0;
+        const int e = whole * UNIT + lane;                  // the last few elements
+        if (e < n1 - n0) {
+            if (F32) reinterpret_cast<unsigned *>(to)[e] = p.Y0 ? reinterpret_cast<const unsigned *>(from)[e] : 0u;
+            else reinterpret_cast<unsigned short *>(to)[e] = p.Y0 ? reinterpret_cast<const unsigned short *>(from)[e] : (unsigned short)0;
         }
     }
 }
@@ -255,7 +256,7 @@ struct Few {
 // permuted alike in both operands.  Second product: 32 columns of Y at a time, MMA i multiplying with rows
 // 8(g / 2) + 2i + g % 2 of B, which leaves lane (g, t) with eight consecutive columns of rows g and g + 8.
 template <int R, bool F32>
-__global__ void __maxnreg__(R <= 64 ? 112 : 232)
+__global__ void __launch_bounds__(FEW_THREADS, R <= 64 ? 2 : 1)
 mwu_adapters_few_kernel(const Params p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     __shared__ union { Finder f; Sorter o; } find;
@@ -293,7 +294,7 @@ mwu_adapters_few_kernel(const Params p) {
         }
         auto row_of = [&](int r) { return rows ? rows[r] : row0 + r; };
         if (a < 0) {
-            copy_rows<F32, 1>(p, row_of, count, ng0 * 32, min(p.rows, ng1 * 32), tid, FEW_THREADS);
+            copy_rows<F32, 2>(p, row_of, count, ng0 * 32, min(p.rows, ng1 * 32), warp, FEW_THREADS / 32);
             continue;
         }
         // this lane's two rows (the first one again where there are fewer: read, never written)
@@ -340,7 +341,7 @@ mwu_adapters_few_kernel(const Params p) {
                 }
             }
         }
-        // the warps' sums, the upper four onto the lower four first (half the memory: a CTA fits beside one of the tile kernel)
+        // the warps' sums, the upper four onto the lower four first: half the memory
         float2 *mine = reinterpret_cast<float2 *>(&sm->red[warp % (FEW_THREADS / 64)][g][2 * t]);
 #pragma unroll
         for (int up = 1; up >= 0; --up) {
@@ -519,38 +520,41 @@ mwu_adapters_few_kernel(const Params p) {
 // ------------------------------------------------------------------------------------------
 // A stage of the first product: 128 rows x 64 columns of X and R x 64 of A.  A chunk of the second: 128 rows x 128 bytes of Y0
 // (64 columns of bf16, 32 of fp32) and as many rows of B.  Both go through the same ring of slots, so the first chunks of Y0 and B come
-// in while T is still being added up.
+// in while T is still being added up, and the next item's first stages while this one's last chunks leave.
+// (Items of 64 rows, a CTA to each and nothing to add up between CTAs: 76 us instead of 54 for 8192 rows, 4096 -> 4096, rank 64; a
+// step of either product takes 0.3 to 0.5 us however few rows it has.)
 // This kernel's clusters hold tensor memory while their CTAs wait for one another.  Were a CTA of another such kernel (on another
 // stream) on the same SM, each could hold what the other waits for; with this much shared memory none fits beside it (the least
-// that such a kernel takes is 36 KB), but a CTA of the kernel for few rows does.
+// that such a kernel takes is 36 KB).
 constexpr int TILE_SMEM = 196 * 1024;
+constexpr int TILE_SLOTS = 8;           // most slots of a ring
+constexpr int TILE_ITEMS = 64;          // most items of a cluster
 
 template <int R, bool F32>
 struct TileCfg {
     static constexpr int TERMS = F32 ? 3 : 2;
     static constexpr int CW = F32 ? 32 : 64;                // columns of Y in a chunk
     static constexpr int BLOCKS = R > 64 ? 2 : 1;           // 64 ranks to a 128-byte row
-    static constexpr int ROWS_BYTES = 128 * 128;
-    static constexpr int SLOT = ROWS_BYTES + 8192 * BLOCKS;
+    static constexpr int ROWS_BYTES = TILE_ROWS * 128;
+    static constexpr int OPERAND = 8192 * BLOCKS;           // of A or B in a slot
     static constexpr int T_BYTES = TERMS * BLOCKS * ROWS_BYTES;
     static constexpr bool POW2 = R > 64 && F32;             // only clusters of 1, 2, 4 or 8 fit
     static constexpr int SUM_BYTES = (POW2 ? 128 : 133) * R * 4;    // of at most 8 CTAs' shares of 128 rows, each rounded up
-    static constexpr int EXTRA = 1024 + 1024;               // alignment, and what TileSmem takes
-    static constexpr int MOST = R > 64 ? 227 * 1024 : TILE_SMEM;
-    static constexpr int FIT = (MOST - EXTRA - T_BYTES - SUM_BYTES) / SLOT;
-    static constexpr int SLOTS = FIT < 6 ? FIT : 6;
-    static constexpr int USED = EXTRA + T_BYTES + SUM_BYTES + SLOTS * SLOT;
-    static constexpr int SMEM = USED < TILE_SMEM ? TILE_SMEM : USED;
-    static_assert(SLOTS >= 2 && SMEM <= 227 * 1024 && 64 * 128 >= CW * 128, "adapter tile kernel: shared memory");
+    static constexpr int EXTRA = 1024 + 2048;               // alignment, and what TileSmem takes
+    static constexpr int SMEM = R > 64 ? 227 * 1024 : TILE_SMEM;
+    static constexpr int SLOT = ROWS_BYTES + OPERAND;
+    static constexpr int ALONE = (SMEM - EXTRA - T_BYTES) / SLOT, TOGETHER = (SMEM - EXTRA - T_BYTES - SUM_BYTES) / SLOT;   // slots of a CTA
+    static_assert(ALONE <= TILE_SLOTS && TOGETHER >= 2, "adapter tile kernel: slots");
 };
 
 struct TileSmem {
-    unsigned long long full[6], empty1[6], empty2[6], tfull1[2], tempty1[2], tfull2[2], tempty2[2], drain;
+    unsigned long long full[TILE_SLOTS], empty[TILE_SLOTS], tfull1[2], tempty1[2], tfull2[2], tempty2[2], drain;
     unsigned tmem_base;
     int abort, drain_abort;
+    int row0[TILE_ITEMS], count[TILE_ITEMS], adapter[TILE_ITEMS];
     Finder f;
 };
-static_assert(sizeof(TileSmem) <= 1024, "adapter tile kernel: shared memory");
+static_assert(sizeof(TileSmem) <= 2048, "adapter tile kernel: shared memory");
 
 __device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int y, int z) {
     asm volatile(
@@ -569,6 +573,35 @@ __device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned (&r)[16]) {
 }
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
+// place in a ring of slots: the slot and how often the ring has been gone round, for its parity
+struct Place {
+    int slot = 0;
+    unsigned round = 0;
+    __device__ __forceinline__ void advance(int by, int slots) {            // by <= slots
+        slot += by;
+        if (slot >= slots) { slot -= slots; ++round; }
+    }
+    __device__ __forceinline__ void retreat(int slots) {
+        if (--slot < 0) { slot += slots; --round; }
+    }
+};
+
+// items cluster, cluster + clusters, ... into the list, by the threads that look after them
+__device__ __forceinline__ void list_items(const Params &p, TileSmem *sm, int per, int first, int cluster, int clusters) {
+    int at = first;
+    for (int s = threadIdx.x * per; s < (int)(threadIdx.x + 1) * per && s < p.segments; ++s) {
+        const int a = __ldg(p.offsets + s), len = __ldg(p.offsets + s + 1) - a, unit = item_rows<false>(p, len);
+        const int n = unit ? (len + unit - 1) / unit : 0;
+        for (int i = at <= cluster ? cluster : cluster + (at - cluster + clusters - 1) / clusters * clusters; i < at + n; i += clusters) {
+            const int k = (i - cluster) / clusters, r = (i - at) * unit;
+            sm->row0[k] = a + r;
+            sm->count[k] = min(unit, len - r);
+            sm->adapter[k] = __ldg(p.which + s);
+        }
+        at += n;
+    }
+}
+
 template <int R, bool F32>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
 mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a,
@@ -576,19 +609,19 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                          const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ Params p) {
     using C = TileCfg<R, F32>;
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *sT = smem_raw + smem_pad_1024(smem_raw);
-    unsigned char *ring = sT + C::T_BYTES;
-    float4 *sums = reinterpret_cast<float4 *>(ring + C::SLOTS * C::SLOT);
-    TileSmem *sm = reinterpret_cast<TileSmem *>(reinterpret_cast<unsigned char *>(sums) + C::SUM_BYTES);
-    volatile int *abort = &sm->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ctas = (int)cluster_size(), c = (int)cluster_rank();
+    const int slots = ctas > 1 ? C::TOGETHER : C::ALONE;
+    unsigned char *ring = smem_raw + smem_pad_1024(smem_raw);
+    unsigned char *sT = ring + slots * C::SLOT;
+    float4 *sums = reinterpret_cast<float4 *>(sT + C::T_BYTES);
+    TileSmem *sm = reinterpret_cast<TileSmem *>(ring + C::SMEM - C::EXTRA);
+    volatile int *abort = &sm->abort;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::SLOTS; ++s) {
+        for (int s = 0; s < TILE_SLOTS; ++s) {
             mbar_init(smem_u32(&sm->full[s]), 1);
-            mbar_init(smem_u32(&sm->empty1[s]), 1);         // released by the first product's MMAs
-            mbar_init(smem_u32(&sm->empty2[s]), 4);         // ... by four warps of the epilogue
+            mbar_init(smem_u32(&sm->empty[s]), 4);          // the four warps of a chunk; a stage's MMAs arrive for all four
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sm->tfull1[b]), 1);
@@ -610,298 +643,351 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
     const int per = (p.segments + TILE_THREADS - 1) / TILE_THREADS;
     int first;
     const int total = count_items<false, TILE_THREADS>(p, &sm->f, per, first);
-    const int item = (int)blockIdx.x / ctas;
-    if (item < total) find_item<false>(p, &sm->f, per, first, item);
+    const int cluster = (int)blockIdx.x / ctas, clusters = (int)gridDim.x / ctas;
+    if (total > 0) list_items(p, sm, per, first, cluster, clusters);
     tc_fence_before();
     __syncthreads();
-    cluster_arrive();                                       // the others may write into this CTA's memory; waited for before the first write
     tc_fence_after();
     const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
-    const bool work = item < total;                         // the whole cluster alike
-    const int row0 = work ? sm->f.row0 : 0, count = work ? sm->f.count : 0, a = work ? sm->f.adapter : -1;
+    const int items = total > cluster ? (total - cluster + clusters - 1) / clusters : 0;    // the whole cluster alike
     const int k_all = (p.cols + 63) / 64, n_all = (p.rows + C::CW - 1) / C::CW;
     const int ks0 = (int)((long long)k_all * c / ctas), ks1 = (int)((long long)k_all * (c + 1) / ctas);
     const int nc0 = (int)((long long)n_all * c / ctas), nc1 = (int)((long long)n_all * (c + 1) / ctas);
-    const int bands = (count + 31) / 32;                    // runs of 32 rows that hold any
     constexpr int PIECE = 8;                                // stages between two sums of T (512 products)
 
-    if (work && a < 0) {
-        copy_rows<F32, 8>(p, [&](int r) { return row0 + r; }, count, nc0 * C::CW, min(p.rows, nc1 * C::CW), threadIdx.x, TILE_THREADS);
-    } else if (work && warp == 0) {
+    // For every item all threads of the cluster meet three times: when all CTAs are done with the item before (1), when the sums
+    // have been given to their owners (2), and when T is with everybody (3).  Every role passes them whether a wait of its own ran
+    // out or not.
+    if (warp == 0) {
         // ---------------- TMA producer ----------------
         bool ok = true;
-        const int n1 = ks1 - ks0, n2 = nc1 - nc0;           // stages and chunks
-        int n = 0;                                          // slots filled so far
-        for (; n < n1; ++n) {
-            const int s = n % C::SLOTS, ks = ks0 + n;
-            if (n >= C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty1[s]), (unsigned)(n / C::SLOTS - 1) & 1u, abort);
-            if (!ok) break;
-            if (elect_one()) {
-                const unsigned bar = smem_u32(&sm->full[s]), dst = smem_u32(ring + s * C::SLOT);
-                mbar_expect_tx(bar, (unsigned)(bands * 4096 + R * 128));
-                for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_x, bar, ks * 64, row0 + 32 * b);
-                tma_load_3d(dst + C::ROWS_BYTES, &tm_a, bar, ks * 64, 0, a);
-            }
-            __syncwarp();
-        }
-        cluster_wait();
-        cluster_arrive();
-        bool waited = false;
-        for (; n < n1 + n2 && ok; ++n) {
-            const int s = n % C::SLOTS, i = nc0 + n - n1;
-            if (n == n1 + C::SLOTS) {                       // slots of the first product are used up; the others need T
-                cluster_wait();
-                cluster_arrive();
-                cluster_wait();
-                waited = true;
-            }
-            if (n >= n1 + C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty2[s]), (unsigned)((n - n1) / C::SLOTS - 1) & 1u, abort);
-            else if (n >= C::SLOTS) ok = warp_wait_spin(smem_u32(&sm->empty1[s]), (unsigned)(n / C::SLOTS - 1) & 1u, abort);
-            if (!ok) break;
-            if (elect_one()) {
-                const unsigned bar = smem_u32(&sm->full[s]), dst = smem_u32(ring + s * C::SLOT);
-                mbar_expect_tx(bar, (unsigned)((p.Y0 ? bands * 4096 : 0) + C::CW * 128 * C::BLOCKS));
-                for (int q = 0; q < C::BLOCKS; ++q)
-                    tma_load_3d(dst + C::ROWS_BYTES + q * C::CW * 128, &tm_b, bar, 64 * q, i * C::CW, a);
-                if (p.Y0)
-                    for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_y0, bar, i * C::CW, row0 + 32 * b);
-            }
-            __syncwarp();
-        }
-        if (!waited) {
-            cluster_wait();
+        Place at;
+#pragma unroll 1
+        for (int it = 0; it < items; ++it) {
+            const int row0 = sm->row0[it], a = sm->adapter[it], bands = (sm->count[it] + 31) / 32;
+            if (a < 0) continue;
             cluster_arrive();
-            cluster_wait();
+            for (int ks = ks0; ok && ks < ks1; ++ks) {
+                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort);
+                if (!ok) break;
+                if (elect_one()) {
+                    const unsigned bar = smem_u32(&sm->full[at.slot]), dst = smem_u32(ring + at.slot * C::SLOT);
+                    mbar_expect_tx(bar, (unsigned)(bands * 4096 + R * 128));
+                    for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_x, bar, ks * 64, row0 + 32 * b);
+                    tma_load_3d(dst + C::ROWS_BYTES, &tm_a, bar, ks * 64, 0, a);
+                }
+                __syncwarp();
+                at.advance(1, slots);
+            }
+            cluster_wait();                                 // (1)
+            cluster_arrive();
+            bool waited = false;
+            for (int i = nc0; ok && i < nc1; ++i) {
+                if (i - nc0 == slots) {                     // from here on a slot comes free only once T is there
+                    cluster_wait();                         // (2)
+                    cluster_arrive();
+                    cluster_wait();                         // (3)
+                    waited = true;
+                }
+                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort);
+                if (!ok) break;
+                if (elect_one()) {
+                    const unsigned bar = smem_u32(&sm->full[at.slot]), dst = smem_u32(ring + at.slot * C::SLOT);
+                    mbar_expect_tx(bar, (unsigned)((p.Y0 ? bands * 4096 : 0) + C::CW * 128 * C::BLOCKS));
+                    for (int q = 0; q < C::BLOCKS; ++q)
+                        tma_load_3d(dst + C::ROWS_BYTES + q * C::CW * 128, &tm_b, bar, 64 * q, i * C::CW, a);
+                    if (p.Y0)
+                        for (int b = 0; b < bands; ++b) tma_load_2d(dst + b * 4096, &tm_y0, bar, i * C::CW, row0 + 32 * b);
+                }
+                __syncwarp();
+                at.advance(1, slots);
+            }
+            if (!waited) {
+                cluster_wait();                             // (2)
+                cluster_arrive();
+                cluster_wait();                             // (3)
+            }
         }
         // a wait ran out: the loads in flight land before this CTA leaves
         if (__any_sync(0xffffffffu, *abort)) {
-            for (int s = 0; s < C::SLOTS; ++s)
-                if (n > s) mbar_wait(smem_u32(&sm->full[s]), (unsigned)((n - s - 1) / C::SLOTS) & 1u, &sm->drain_abort);
+            for (int s = 0; s < slots; ++s)
+                if (at.round || s < at.slot)                // this slot's latest load
+                    mbar_wait(smem_u32(&sm->full[s]), (s < at.slot ? at.round : at.round - 1u) & 1u, &sm->drain_abort);
             __syncwarp();
         }
-    } else if (work && warp == 1) {
+    } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         bool ok = true;
-        int n = 0;
-        unsigned use = 0;
-        for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
-            ok = warp_wait_spin(smem_u32(&sm->tempty1[use & 1u]), ((use >> 1) & 1u) ^ 1u, abort);
-            if (!ok) break;
-            tc_fence_after();
-            const int k1 = min(ks1, k0 + PIECE);
-            for (int ks = k0; ks < k1; ++ks, ++n) {
-                const int s = n % C::SLOTS;
-                ok = warp_wait_spin(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort);
+        Place at;
+        unsigned use = 0, used2 = 0;                        // uses of the first product's accumulators; bit b: parity of those of the second's b
+#pragma unroll 1
+        for (int it = 0; it < items; ++it) {
+            if (sm->adapter[it] < 0) continue;
+            cluster_arrive();
+            for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
+                ok = warp_wait_spin(smem_u32(&sm->tempty1[use & 1u]), ((use >> 1) & 1u) ^ 1u, abort);
                 if (!ok) break;
                 tc_fence_after();
-                if (elect_one()) {
-                    const unsigned long long xd = make_desc(smem_u32(ring + s * C::SLOT));
-                    const unsigned long long ad = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES));
+                const int k1 = min(ks1, k0 + PIECE);
+                for (int ks = k0; ks < k1; ++ks, at.advance(1, slots)) {
+                    const int s = at.slot;
+                    ok = warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const unsigned long long xd = make_desc(smem_u32(ring + s * C::SLOT));
+                        const unsigned long long ad = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES));
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4)
-                        umma_bf16(tmem_base + (use & 1u) * R, xd + 2ull * k4, ad + 2ull * k4, make_idesc(R), (ks > k0 || k4) ? 1u : 0u);
-                    umma_commit(smem_u32(&sm->empty1[s]));
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            umma_bf16(tmem_base + (use & 1u) * R, xd + 2ull * k4, ad + 2ull * k4, make_idesc(R), (ks > k0 || k4) ? 1u : 0u);
+                        for (int i = 0; i < 3; ++i) mbar_arrive(smem_u32(&sm->empty[s]));
+                        umma_commit(smem_u32(&sm->empty[s]));
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (elect_one()) umma_commit(smem_u32(&sm->tfull1[use & 1u]));
+                __syncwarp();
+            }
+            cluster_wait();                                 // (1)
+            cluster_arrive();
+            cluster_wait();                                 // (2)
+            cluster_arrive();
+            cluster_wait();                                 // (3): T of all rows is here, as bf16 terms
+            fence_proxy_async_all();
+            for (int j = 0; ok && j < nc1 - nc0; ++j, at.advance(1, slots)) {
+                const int s = at.slot;
+                const unsigned buf = (unsigned)j & 1u;
+                ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((used2 >> buf) & 1u) ^ 1u, abort) &&
+                     warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort);
+                if (!ok) break;
+                used2 ^= 1u << buf;
+                tc_fence_after();
+                if (elect_one()) {
+                    unsigned acc = 0;
+#pragma unroll
+                    for (int q = C::TERMS - 1; q >= 0; --q) // the smallest term first
+#pragma unroll
+                        for (int r = 0; r < R / 16; ++r) {
+                            const unsigned long long td = make_desc(smem_u32(sT + (q * C::BLOCKS + r / 4) * C::ROWS_BYTES));
+                            const unsigned long long bd = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES + (r / 4) * C::CW * 128));
+                            umma_bf16(tmem_base + 256u + buf * 64u, td + 2ull * (r % 4), bd + 2ull * (r % 4), make_idesc(C::CW), acc);
+                            acc = 1;
+                        }
+                    umma_commit(smem_u32(&sm->tfull2[buf]));
                 }
                 __syncwarp();
             }
-            if (!ok) break;
-            if (elect_one()) umma_commit(smem_u32(&sm->tfull1[use & 1u]));
-            __syncwarp();
-        }
-        cluster_wait();
-        cluster_arrive();
-        cluster_wait();
-        cluster_arrive();
-        cluster_wait();                                     // T of all rows is here, as bf16 terms
-        fence_proxy_async_all();
-        n = ks1 - ks0;
-        for (int j = 0; ok && j < nc1 - nc0; ++j, ++n) {
-            const int s = n % C::SLOTS;
-            const unsigned buf = (unsigned)j & 1u;
-            ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((unsigned)(j >> 1) & 1u) ^ 1u, abort) &&
-                 warp_wait_spin(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                unsigned acc = 0;
-#pragma unroll
-                for (int q = C::TERMS - 1; q >= 0; --q)     // the smallest term first
-#pragma unroll
-                    for (int r = 0; r < R / 16; ++r) {
-                        const unsigned long long td = make_desc(smem_u32(sT + (q * C::BLOCKS + r / 4) * C::ROWS_BYTES));
-                        const unsigned long long bd = make_desc(smem_u32(ring + s * C::SLOT + C::ROWS_BYTES + (r / 4) * C::CW * 128));
-                        umma_bf16(tmem_base + 256u + buf * 64u, td + 2ull * (r % 4), bd + 2ull * (r % 4), make_idesc(C::CW), acc);
-                        acc = 1;
-                    }
-                umma_commit(smem_u32(&sm->tfull2[buf]));
-            }
-            __syncwarp();
         }
         // everything this thread issued must have retired before tensor memory is freed
         if (elect_one()) umma_commit(smem_u32(&sm->drain));
         __syncwarp();
         mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort);
         __syncwarp();
-    } else if (work) {
+    } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane, tid = threadIdx.x - 64;
-        bool ok = true;
-        // ---------------- T of this CTA's slice, to shared memory ----------------
         constexpr int MINE = R >= 64 ? R / 2 : R;           // columns of T a warp takes (up to 32 ranks: the first four warps)
         constexpr int LD = MINE < 32 ? 16 : 32;
         const int col0 = R >= 64 ? half * MINE : 0;
-        float t[MINE];
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) t[j] = 0.f;
-        unsigned use = 0;
-        for (int k0 = ks0; k0 < ks1; k0 += PIECE, ++use) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull1[use & 1u]), (use >> 1) & 1u, abort));
-            if (!ok) break;
-            tc_fence_after();
-            if (R >= 64 || half == 0) {
-#pragma unroll
-                for (int q = 0; q < MINE / LD; ++q) {
-                    unsigned v[LD];
-                    const unsigned at = tmem_base + ((unsigned)(quarter * 32) << 16) + (use & 1u) * R + (unsigned)(col0 + q * LD);
-                    if constexpr (LD == 16) tmem_ld16(at, v);
-                    else tmem_ld32(at, v);
-#pragma unroll
-                    for (int j = 0; j < LD; ++j) t[q * LD + j] += __uint_as_float(v[j]);
-                }
+        const bool has_t = R >= 64 || half == 0;
+        bool ok = true;
+        Place at;                                           // of the chunk in hand (its stages' slots are skipped)
+        unsigned use = 0, used2 = 0;
+#pragma unroll 1
+        for (int it = 0; it < items; ++it) {
+            const int row0 = sm->row0[it], count = sm->count[it], a = sm->adapter[it];
+            if (a < 0) {
+                copy_rows<F32, 8>(p, [&](int r) { return row0 + r; }, count, nc0 * C::CW, min(p.rows, nc1 * C::CW), warp - 2, 8);
+                __syncwarp();
+                continue;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sm->tempty1[use & 1u]));
-        }
-        // To the CTA that adds up this row: [CTA it comes from][four ranks][row], 16 bytes each, rows next to one another.
-        const int owner = ((row + 1) * ctas - 1) / 128, most = (128 + ctas - 1) / ctas;
-        const unsigned there = smem_u32(sums + (c * (R / 4) + col0 / 4) * most + row - 128 * owner / ctas);
-        cluster_wait();                                     // all CTAs are there
-        if (R >= 64 || half == 0) {
-            unsigned at;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(there), "r"(owner));
+            cluster_arrive();
+            // ---------------- T of this CTA's slice ----------------
+            float t[MINE];
 #pragma unroll
-            for (int j = 0; j < MINE / 4; ++j)
-                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
-                             ::"r"(at + (unsigned)(j * most * 16)), "f"(t[4 * j]), "f"(t[4 * j + 1]), "f"(t[4 * j + 2]), "f"(t[4 * j + 3]) : "memory");
-        }
-        cluster_arrive();
-        cluster_wait();
-        // ---------------- this CTA's share of the rows: added up, scaled, split, given to all ----------------
-        const int r0 = 128 * c / ctas, nr = 128 * (c + 1) / ctas - r0;
-        const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
-        for (int e = tid; e < nr * (R / 8); e += 256) {
-            const int rr = e % nr, q8 = e / nr, r = r0 + rr;
-            float f[8];
+            for (int j = 0; j < MINE; ++j) t[j] = 0.f;
+            for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull1[use & 1u]), (use >> 1) & 1u, abort));
+                if (!ok) break;
+                tc_fence_after();
+                if (has_t) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int o = 0; o < ctas; ++o) {
-                    const float4 v = sums[(o * (R / 4) + 2 * q8 + h) * most + rr];
-                    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+                    for (int q = 0; q < MINE / LD; ++q) {
+                        unsigned v[LD];
+                        const unsigned at = tmem_base + ((unsigned)(quarter * 32) << 16) + (use & 1u) * R + (unsigned)(col0 + q * LD);
+                        if constexpr (LD == 16) tmem_ld16(at, v);
+                        else tmem_ld32(at, v);
+#pragma unroll
+                        for (int j = 0; j < LD; ++j) t[q * LD + j] += __uint_as_float(v[j]);
+                    }
                 }
-                f[4 * h] = s.x * scale; f[4 * h + 1] = s.y * scale; f[4 * h + 2] = s.z * scale; f[4 * h + 3] = s.w * scale;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm->tempty1[use & 1u]));
             }
-            const unsigned place = smem_u32(sT) + (unsigned)(q8 / 8) * C::ROWS_BYTES + swz((unsigned)r, (unsigned)q8 & 7u);
+            const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
+            // eight ranks of a row, scaled, as bf16 terms, to T of CTAs o0 .. o1 - 1
+            auto give = [&](float (&f)[8], int r, int q8, int o0, int o1) {
+                const unsigned place = smem_u32(sT) + (unsigned)(q8 / 8) * C::ROWS_BYTES + swz((unsigned)r, (unsigned)q8 & 7u);
 #pragma unroll
-            for (int q = 0; q < C::TERMS; ++q) {
-                unsigned w[4];
+                for (int j = 0; j < 8; ++j) f[j] *= scale;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-                    w[j] = *reinterpret_cast<const unsigned *>(&h);
-                    f[2 * j] -= __low2float(h);
-                    f[2 * j + 1] -= __high2float(h);
+                for (int q = 0; q < C::TERMS; ++q) {
+                    unsigned w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+                        w[j] = *reinterpret_cast<const unsigned *>(&h);
+                        f[2 * j] -= __low2float(h);
+                        f[2 * j + 1] -= __high2float(h);
+                    }
+#pragma unroll 1
+                    for (int o = o0; o < o1; ++o) {
+                        unsigned at;
+                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(place + (unsigned)(q * C::BLOCKS * C::ROWS_BYTES)), "r"(o));
+                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
                 }
-                for (int o = 0; o < ctas; ++o) {
-                    unsigned at;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(place + (unsigned)(q * C::BLOCKS * C::ROWS_BYTES)), "r"(o));
-                    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                }
+            };
+            // To the CTA that adds up this row: [CTA it comes from][four ranks][row], 16 bytes each, rows next to one another.
+            const int owner = ((row + 1) * ctas - 1) / 128, most = (128 + ctas - 1) / ctas;
+            const unsigned there = smem_u32(sums + (c * (R / 4) + col0 / 4) * most + row - 128 * owner / ctas);
+            cluster_wait();                                 // (1)
+            if (ctas > 1 && has_t) {
+                unsigned at;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(there), "r"(owner));
+#pragma unroll
+                for (int j = 0; j < MINE / 4; ++j)
+                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                                 ::"r"(at + (unsigned)(j * most * 16)), "f"(t[4 * j]), "f"(t[4 * j + 1]), "f"(t[4 * j + 2]), "f"(t[4 * j + 3]) : "memory");
             }
-        }
-        fence_proxy_async_all();
-        cluster_arrive();
-        cluster_wait();
-        // ---------------- chunks of Y: four warps take the even ones, four the odd ones ----------------
-        const int rows_here = min(32, max(0, count - quarter * 32));
-        for (int j = half; ok && j < nc1 - nc0; j += 2) {
-            const int i = nc0 + j, n = ks1 - ks0 + j, s = n % C::SLOTS;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), (unsigned)(j >> 1) & 1u, abort) &&
-                                             mbar_wait(smem_u32(&sm->full[s]), (unsigned)(n / C::SLOTS) & 1u, abort));
-            if (!ok) break;
-            tc_fence_after();
-            unsigned v[C::CW / 32][32];
+            cluster_arrive();
+            cluster_wait();                                 // (2)
+            if (ctas == 1) {
+                if (has_t) {
 #pragma unroll
-            for (int q = 0; q < C::CW / 32; ++q)
-                tmem_ld32(tmem_base + ((unsigned)(quarter * 32) << 16) + 256u + (unsigned)(half * 64 + q * 32), v[q]);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sm->tempty2[half]));
-            unsigned char *box = ring + s * C::SLOT + quarter * 4096;
-            const int n0 = i * C::CW;
-            if (rows_here > 0) {
+                    for (int j = 0; j < MINE / 8; ++j) {
+                        float f[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + ((j ^ (lane & 7)) << 4));
-                    uint4 y = p.Y0 ? *at : make_uint4(0, 0, 0, 0);
-                    if (F32) {
-                        y.x = __float_as_uint(__uint_as_float(y.x) + __uint_as_float(v[0][4 * j]));
-                        y.y = __float_as_uint(__uint_as_float(y.y) + __uint_as_float(v[0][4 * j + 1]));
-                        y.z = __float_as_uint(__uint_as_float(y.z) + __uint_as_float(v[0][4 * j + 2]));
-                        y.w = __float_as_uint(__uint_as_float(y.w) + __uint_as_float(v[0][4 * j + 3]));
-                    } else {
-                        unsigned w[4] = {y.x, y.y, y.z, y.w};
+                        for (int e = 0; e < 8; ++e) f[e] = t[8 * j + e];
+                        give(f, row, col0 / 8 + j, 0, 1);
+                    }
+                }
+            } else {
+                // this CTA's share of the rows: added up and given to all
+                const int r0 = 128 * c / ctas, nr = 128 * (c + 1) / ctas - r0;
+#pragma unroll 1
+                for (int e = tid; e < nr * (R / 8); e += 256) {
+                    const int rr = e % nr, q8 = e / nr;
+                    float f[8];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int e = 8 * j + 2 * q;
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[q] << 16) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32]),
-                                                                           __uint_as_float(w[q] & 0xffff0000u) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32 + 1]));
-                            w[q] = *reinterpret_cast<const unsigned *>(&h);
+                    for (int h = 0; h < 2; ++h) {
+                        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                        for (int o = 0; o < ctas; ++o) {
+                            const float4 v = sums[(o * (R / 4) + 2 * q8 + h) * most + rr];
+                            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
                         }
-                        y = make_uint4(w[0], w[1], w[2], w[3]);
+                        f[4 * h] = s.x; f[4 * h + 1] = s.y; f[4 * h + 2] = s.z; f[4 * h + 3] = s.w;
                     }
-                    *at = y;
+                    give(f, r0 + rr, q8, 0, ctas);
                 }
-                // Whole boxes, clipped at the last column by the map, which clips a store at 16 bytes only.
-                if (rows_here == 32 && (n0 + C::CW <= p.rows || p.rows % (C::CW / 8) == 0)) {
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_2d(&tm_y, smem_u32(box), n0, row0 + quarter * 32);
-                        bulk_commit();
-                        bulk_wait_read();
+            }
+            fence_proxy_async_all();
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();                                 // (3)
+            // ---------------- chunks of Y: four warps take the even ones, four the odd ones ----------------
+            const int rows_here = min(32, max(0, count - quarter * 32));
+            at.round += (unsigned)(ks1 - ks0) / slots;
+            at.advance((ks1 - ks0) % slots + half, slots);
+#pragma unroll 1
+            for (int j = half; ok && j < nc1 - nc0; j += 2, ++used2, at.advance(2, slots)) {
+                const int i = nc0 + j, s = at.slot;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), used2 & 1u, abort) &&
+                                                 mbar_wait(smem_u32(&sm->full[s]), at.round & 1u, abort));
+                if (!ok) break;
+                tc_fence_after();
+                unsigned v[C::CW / 32][32];
+                if (rows_here > 0) {
+#pragma unroll
+                    for (int q = 0; q < C::CW / 32; ++q)
+                        tmem_ld32(tmem_base + ((unsigned)(quarter * 32) << 16) + 256u + (unsigned)(half * 64 + q * 32), v[q]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm->tempty2[half]));
+                unsigned char *box = ring + s * C::SLOT + quarter * 4096;
+                const int n0 = i * C::CW;
+                if (rows_here > 0) {
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        uint4 *at = reinterpret_cast<uint4 *>(box + lane * 128 + ((g ^ (lane & 7)) << 4));
+                        uint4 y = p.Y0 ? *at : make_uint4(0, 0, 0, 0);
+                        if (F32) {
+                            y.x = __float_as_uint(__uint_as_float(y.x) + __uint_as_float(v[0][4 * g]));
+                            y.y = __float_as_uint(__uint_as_float(y.y) + __uint_as_float(v[0][4 * g + 1]));
+                            y.z = __float_as_uint(__uint_as_float(y.z) + __uint_as_float(v[0][4 * g + 2]));
+                            y.w = __float_as_uint(__uint_as_float(y.w) + __uint_as_float(v[0][4 * g + 3]));
+                        } else {
+                            unsigned w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int e = 8 * g + 2 * q;
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(w[q] << 16) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32]),
+                                                                               __uint_as_float(w[q] & 0xffff0000u) + __uint_as_float(v[e / 32 % (C::CW / 32)][e % 32 + 1]));
+                                w[q] = *reinterpret_cast<const unsigned *>(&h);
+                            }
+                            y = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        *at = y;
                     }
-                } else {                                    // the rows behind are another segment's, the columns behind the caller's
-                    __syncwarp();
-                    for (int b = 0; b < rows_here; b += 4) {
-                        const int r = b + (lane >> 3), j = lane & 7, left = p.rows - n0 - j * (C::CW / 8);
-                        if (r < rows_here && left > 0) {
-                            const uint4 y = *reinterpret_cast<const uint4 *>(box + r * 128 + ((j ^ (r & 7)) << 4));
-                            const long long at = (long long)(row0 + quarter * 32 + r) * p.ldy + n0 + j * (C::CW / 8);
-                            if (left >= C::CW / 8) {
-                                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.Y) + at * (F32 ? 4 : 2)) = y;
-                            } else {
-                                const unsigned w[4] = {y.x, y.y, y.z, y.w};
-                                for (int e = 0; e < left; ++e) {
-                                    if (F32) reinterpret_cast<unsigned *>(p.Y)[at + e] = e == 0 ? w[0] : e == 1 ? w[1] : w[2];
-                                    else {
-                                        const unsigned u = e < 2 ? w[0] : e < 4 ? w[1] : e < 6 ? w[2] : w[3];
-                                        reinterpret_cast<unsigned short *>(p.Y)[at + e] = (unsigned short)(e & 1 ? u >> 16 : u);
+                    // Whole boxes, clipped at the last column by the map, which clips a store at 16 bytes only.
+                    if (rows_here == 32 && (n0 + C::CW <= p.rows || p.rows % (C::CW / 8) == 0)) {
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&tm_y, smem_u32(box), n0, row0 + quarter * 32);
+                        }
+                    } else {                                    // the rows behind are another segment's, the columns behind the caller's
+                        __syncwarp();
+                        for (int b = 0; b < rows_here; b += 4) {
+                            const int r = b + (lane >> 3), g = lane & 7, left = p.rows - n0 - g * (C::CW / 8);
+                            if (r < rows_here && left > 0) {
+                                const uint4 y = *reinterpret_cast<const uint4 *>(box + r * 128 + ((g ^ (r & 7)) << 4));
+                                const long long at = (long long)(row0 + quarter * 32 + r) * p.ldy + n0 + g * (C::CW / 8);
+                                if (left >= C::CW / 8) {
+                                    *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.Y) + at * (F32 ? 4 : 2)) = y;
+                                } else {
+                                    const unsigned w[4] = {y.x, y.y, y.z, y.w};
+                                    for (int e = 0; e < left; ++e) {
+                                        if (F32) reinterpret_cast<unsigned *>(p.Y)[at + e] = e == 0 ? w[0] : e == 1 ? w[1] : w[2];
+                                        else {
+                                            const unsigned u = e < 2 ? w[0] : e < 4 ? w[1] : e < 6 ? w[2] : w[3];
+                                            reinterpret_cast<unsigned short *>(p.Y)[at + e] = (unsigned short)(e & 1 ? u >> 16 : u);
+                                        }
                                     }
                                 }
                             }
                         }
                     }
                 }
+                if (lane == 0) {
+                    bulk_commit();
+                    bulk_wait_read();                       // (a slot given back a chunk later, unread stores or not: 54 us instead of 50)
+                    mbar_arrive(smem_u32(&sm->empty[s]));
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sm->empty2[s]));
+            // on to the first slot behind this item's chunks
+            if (half) {
+                if ((nc1 - nc0) % 2 == 0) at.retreat(slots);
+            } else if ((nc1 - nc0) % 2) at.retreat(slots);
         }
         if (lane == 0) bulk_wait_all();
         __syncwarp();
     }
 
-    if (!work || a < 0) cluster_wait();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -947,6 +1033,35 @@ static bool encode(CUtensorMap *tm, const void *ptr, bool fp32, int64_t inner, i
                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// clusters of `ctas` CTAs of the tile kernel that this device runs at a time: a fact of the device, asked once for each
+template <int R, bool F32>
+static long long clusters_at_once(int ctas, int sm_count) {
+    constexpr int DEVICES = 64;
+    static std::atomic<int> known[DEVICES][9];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= DEVICES) return sm_count / ctas;
+    int n = known[dev][ctas].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ctas;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(TILE_THREADS);
+        cfg.dynamicSmemBytes = TileCfg<R, F32>::SMEM;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, mwu_adapters_tile_kernel<R, F32>, &cfg) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            n = sm_count / ctas;
+        }
+        known[dev][ctas].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <int R, bool F32>
 static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
     auto kern = mwu_adapters_tile_kernel<R, F32>;
@@ -954,20 +1069,33 @@ static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
     constexpr int smem = C::SMEM;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MWU_ERR_CUDA;
     if (!get_encode_fn()) return MWU_ERR_CUDA;
+    // CTAs of a cluster: what an estimate in microseconds says, of the items that are to be expected (half of the segments that may be long
+    // are).  A round takes what it takes to begin and to add up T, and a CTA's share of X, Y0, Y, A and B at 50 GB/s.  Any choice gives every
+    // row its adapter.  (8192 rows, 4096 -> 4096, rank 64: two 50 us, four 55; 2777 rows of prompts, 1216 -> 1000, fp32: four 20.2, two
+    // 22.5, eight 25.)
+    const long long longer = p.M / (FEW_ROWS + 1), some = longer < p.segments ? longer : p.segments;
+    const long long expected = (p.M + TILE_ROWS - 1) / TILE_ROWS + (some < p.M / 256 ? some : p.M / 256) / 2;
+    const double size = F32 ? 4 : 2;
+    const double item = TILE_ROWS * (2.0 * p.cols + (p.Y0 ? 2.0 : 1.0) * size * p.rows) + 2.0 * p.rank * ((double)p.rows + p.cols);
+    double best = 1e30;
+    int ctas = 1;
+    for (int n = 1; n <= 8; ++n) {
+        if (C::POW2 && (n & (n - 1))) continue;
+        const long long places = clusters_at_once<R, F32>(n, sm_count), rounds = (expected + places - 1) / places;
+        const double us = rounds * ((n > 1 ? 6.0 : 4.0) + item / n / 50e3);
+        if (us < 0.97 * best) { best = us; ctas = n; }
+    }
+    const long long most = p.M / TILE_ROWS + some, places = clusters_at_once<R, F32>(ctas, sm_count);
+    long long clusters = most < places ? most : places;
+    if (clusters < (most + TILE_ITEMS - 1) / TILE_ITEMS) clusters = (most + TILE_ITEMS - 1) / TILE_ITEMS;
     CUtensorMap tm_x, tm_a, tm_b, tm_y0, tm_y;
     if (!encode(&tm_x, p.X, false, p.cols, p.M, p.ldx, 32, 0, 0) || !encode(&tm_a, p.A, false, p.cols, p.rank, p.lda, R, p.adapters, p.a_stride) ||
-        !encode(&tm_b, p.B, false, p.rank, p.rows, p.ldb, C::CW, p.adapters, p.b_stride) || !encode(&tm_y, p.Y, F32, p.rows, p.M, p.ldy, 32, 0, 0) ||
-        !encode(&tm_y0, p.Y0 ? p.Y0 : p.Y, F32, p.rows, p.M, p.ldy, 32, 0, 0))
+        !encode(&tm_b, p.B, false, p.rank, p.rows, p.ldb, C::CW, p.adapters, p.b_stride) || !encode(&tm_y, p.Y, F32, p.rows, p.M, p.ldy, 32, 0, 0))
         return MWU_ERR_CUDA;
-    // Longer segments than FEW_ROWS have an item for every 128 rows and one that is not full.  The cluster is as large as keeps
-    // what is to be expected (half of the segments full ones) in one round; any size gives every row its adapter.
-    const long long longer = p.M / (FEW_ROWS + 1), some = longer < p.segments ? longer : p.segments;
-    const long long most = p.M / 128 + some, expected = (p.M + 127) / 128 + (some < p.M / 256 ? some : p.M / 256);
-    long long ctas = sm_count / expected;
-    ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
-    if (C::POW2) ctas = ctas >= 8 ? 8 : ctas >= 4 ? 4 : ctas >= 2 ? 2 : 1;
+    tm_y0 = tm_y;                                           // without Y0 it is not used
+    if (p.Y0 && p.Y0 != p.Y && !encode(&tm_y0, p.Y0, F32, p.rows, p.M, p.ldy, 32, 0, 0)) return MWU_ERR_CUDA;
     count_launch();
-    return launch_chained(kern, dim3((unsigned)(most * ctas)), dim3(TILE_THREADS), smem, st, (int)ctas, tm_x, tm_a, tm_b, tm_y0, tm_y, p) ==
+    return launch_chained(kern, dim3((unsigned)(clusters * ctas)), dim3(TILE_THREADS), smem, st, ctas, tm_x, tm_a, tm_b, tm_y0, tm_y, p) ==
                    cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
 }
 
