@@ -38,7 +38,6 @@ constexpr int G_THREADS = 32 * (3 + G_EPI_WARPS);
 constexpr int G_SIDE = 128 * 128;                    // bytes of one operand of a stage in one CTA: 128 features or lines x 64
 constexpr int G_STAGE_BYTES = 2 * G_SIDE;
 constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 64 reduction steps
-constexpr int G_LINE_BOX = 32;                       // lines of a K-major box
 constexpr int G_BAND = 8;                            // line tiles per band of the tile order
 constexpr int G_CHUNK = 8;                           // stages between two sums of an fp32 result (512 products)
 
@@ -54,6 +53,11 @@ struct GroupedParams {
     int out_fp32, accumulate;
     unsigned *dev_status;
 };
+
+// The lines of a CTA's half tile as few boxes, whose issue takes as long as some of their transfer: 128 lines (from 97 on; what is
+// too many is never multiplied), 64 and 32, 64, or 32.  A weight gradient's boxes are 64 lines wide by 64 rows and take only m[0].
+struct LineMaps { CUtensorMap m[3]; };
+__device__ __forceinline__ int boxed_lines(int half) { return half > 96 ? 128 : (half + 31) & ~31; }
 
 struct GroupedSmem {
     unsigned long long full[G_STAGES], empty[G_STAGES], tail[G_STAGES], peer_fixed[G_STAGES], tfull[2], tempty[2], drain;
@@ -151,7 +155,7 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams &p, const Group
 
 template <int OP>
 __global__ void __launch_bounds__(G_THREADS, 1)
-mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ CUtensorMap tmap_l,
+mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ LineMaps maps_l,
                         const __grid_constant__ GroupedParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *sF = smem_raw + smem_pad_1024(smem_raw);
@@ -235,8 +239,8 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
             grouped_tile<OP>(p, sm, k, f_tiles, t);
             const int n_st = (t.red_len + 63) / 64, half = t.line_pad / 2;
             const int f0 = t.feature0 + (int)rank * 128, l0 = t.line0 + (int)rank * half;
-            const int boxes = OP == G_DW ? (half + 63) / 64 : (half + G_LINE_BOX - 1) / G_LINE_BOX;
-            const unsigned bytes = (unsigned)G_SIDE + (unsigned)boxes * (OP == G_DW ? G_SUB : G_LINE_BOX * 128);
+            const int boxes = (half + 63) / 64, boxed = boxed_lines(half);
+            const unsigned bytes = (unsigned)G_SIDE + (OP == G_DW ? (unsigned)boxes * G_SUB : (unsigned)boxed * 128u);
             for (int ks = 0; ks < n_st; ++ks) {
                 if (!mbar_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort)) ok = false;
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -251,7 +255,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                         mbar_expect_tx(bar, bytes);
                         tma_load_2d(df, &tmap_f, bar, f0, t.red0 + r0);
                         tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
-                        for (int b = 0; b < boxes; ++b) tma_load_2d(dl + b * G_SUB, &tmap_l, bar, l0 + 64 * b, t.red0 + r0);
+                        for (int b = 0; b < boxes; ++b) tma_load_2d(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
                     } else {
                         const unsigned bar = mbar_addr_in_cta(smem_u32(&sm->full[stage]), 0);
                         if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), 2 * bytes);
@@ -264,9 +268,12 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                             tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
                             tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
                         }
-                        for (int b = 0; b < boxes; ++b) {
-                            if (OP == G_DW) tma_load_2d_pair(dl + b * G_SUB, &tmap_l, bar, l0 + 64 * b, t.red0 + r0);
-                            else tma_load_2d_pair(dl + b * G_LINE_BOX * 128, &tmap_l, bar, r0, l0 + G_LINE_BOX * b);
+                        if (OP == G_DW) {
+                            for (int b = 0; b < boxes; ++b) tma_load_2d_pair(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
+                        } else {
+                            if (boxed == 128) tma_load_2d_pair(dl, &maps_l.m[0], bar, r0, l0);
+                            else if (boxed & 64) tma_load_2d_pair(dl, &maps_l.m[1], bar, r0, l0);
+                            if (boxed & 32) tma_load_2d_pair(dl + (boxed & 64) * 128, &maps_l.m[2], bar, r0, l0 + (boxed & 64));
                         }
                     }
                 }
@@ -439,7 +446,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
 }
 
 template <int OP>
-static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const CUtensorMap &tmap_l, const GroupedParams &p, long long most_tiles,
+static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const GroupedParams &p, long long most_tiles,
                                   int sm_count, cudaStream_t st) {
     auto kern = mwu_gemm_grouped_kernel<OP>;
     const size_t smem = 1024 + (size_t)G_STAGES * G_STAGE_BYTES + sizeof(GroupedSmem);
@@ -447,7 +454,7 @@ static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const CUtensorMap &
     if (e != cudaSuccess) return e;
     const long long pairs = most_tiles < sm_count / 2 ? most_tiles : sm_count / 2;
     count_launch();
-    return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, tmap_l, p);
+    return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, maps_l, p);
 }
 
 // box of 64 elements of the contiguous axis by `box_rows`, one group
@@ -492,11 +499,12 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     if (M == 0) return MWU_OK;
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
-    CUtensorMap tmap_f, tmap_l;
-    if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? 128 : 64, groups, w_stride) ||
-        !encode_bf16(encode, &tmap_l, in, red, M, ldi, G_LINE_BOX, 0, 0))
-        return MWU_ERR_CUDA;
-    return launch_grouped<OP>(tmap_f, tmap_l, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+    CUtensorMap tmap_f;
+    LineMaps maps_l;
+    if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? 128 : 64, groups, w_stride)) return MWU_ERR_CUDA;
+    for (int b = 0; b < 3; ++b)
+        if (!encode_bf16(encode, &maps_l.m[b], in, red, M, ldi, 128 >> b, 0, 0)) return MWU_ERR_CUDA;
+    return launch_grouped<OP>(tmap_f, maps_l, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
 }
 
 }  // namespace gemm
@@ -543,9 +551,11 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     if (rc != MWU_OK) return rc;
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
-    CUtensorMap tmap_f, tmap_l;
+    CUtensorMap tmap_f;
+    LineMaps maps_l;
     const int64_t m_rows = M > 0 ? M : 1;               // no rows: the maps are never used, the gradients are zeros
-    if (!encode_bf16(encode, &tmap_f, X, cols, m_rows, ldx, 64, 0, 0) || !encode_bf16(encode, &tmap_l, dY, rows, m_rows, lddy, 64, 0, 0))
+    if (!encode_bf16(encode, &tmap_f, X, cols, m_rows, ldx, 64, 0, 0) || !encode_bf16(encode, &maps_l.m[0], dY, rows, m_rows, lddy, 64, 0, 0))
         return MWU_ERR_CUDA;
-    return launch_grouped<G_DW>(tmap_f, tmap_l, p, tiles, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+    maps_l.m[1] = maps_l.m[2] = maps_l.m[0];
+    return launch_grouped<G_DW>(tmap_f, maps_l, p, tiles, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
 }
