@@ -31,13 +31,14 @@ namespace gemm {
 
 EncodeTiledFn get_encode_fn();          // mwu_gemm.cu
 
-constexpr int G_STAGES = 6;
+constexpr int G_STAGES = 5;
 constexpr int G_EPI_WARPS = 8;
 constexpr int G_FIX_WARP = 2 + G_EPI_WARPS;
 constexpr int G_THREADS = 32 * (3 + G_EPI_WARPS);
 constexpr int G_SIDE = 128 * 128;                    // bytes of one operand of a stage in one CTA: 128 features or lines x 64
 constexpr int G_STAGE_BYTES = 2 * G_SIDE;
 constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 64 reduction steps
+constexpr int G_BOX = 2048;                          // of output: 32 features x 16 lines of fp32, x 32 of bf16; two to a warp
 constexpr int G_BAND = 8;                            // line tiles per band of the tile order
 constexpr int G_CHUNK = 8;                           // stages between two sums of an fp32 result (512 products)
 
@@ -69,13 +70,21 @@ struct GroupedSmem {
     unsigned short live[MWU_MAX_GROUPS];
 };
 
-static_assert(1024 + G_STAGES * G_STAGE_BYTES + sizeof(GroupedSmem) <= 232448, "grouped kernel: shared memory above 227 KB");
+static_assert(1024 + G_STAGES * G_STAGE_BYTES + G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem) <= 232448, "grouped kernel: shared memory above 227 KB");
 
 __device__ __forceinline__ void tma_load_3d_pair(unsigned dst, const CUtensorMap *map, unsigned bar_cluster, int x, int y, int z) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 "
         "[%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(bar_cluster), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap *map, unsigned src, int x, int y, int z) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
 }
 // MN-major operand, 128-byte swizzle: 64 features to a row of 128 bytes, 8 reduction steps to 1024 bytes, the next 64 features
 // G_SUB bytes on
@@ -156,11 +165,12 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams &p, const Group
 template <int OP>
 __global__ void __launch_bounds__(G_THREADS, 1)
 mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ LineMaps maps_l,
-                        const __grid_constant__ GroupedParams p) {
+                        const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ GroupedParams p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *sF = smem_raw + smem_pad_1024(smem_raw);
     unsigned char *sL = sF + G_STAGES * G_SIDE;
-    GroupedSmem *sm = reinterpret_cast<GroupedSmem *>(sL + G_STAGES * G_SIDE);
+    unsigned char *boxes_out = sL + G_STAGES * G_SIDE;
+    GroupedSmem *sm = reinterpret_cast<GroupedSmem *>(boxes_out + G_EPI_WARPS * 2 * G_BOX);
     volatile int *abort = &sm->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = cluster_rank();               // 0: leader (issues the MMAs), 1: peer
@@ -374,6 +384,26 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         const int odd = (warp - 2) >> 2;                    // its share: every other 32 lines
         unsigned use = 0;
         bool ok = true;
+        unsigned char *stg = boxes_out + (warp - 2) * 2 * G_BOX;
+        unsigned box_at = 0;
+        const unsigned box_flip = G_BOX;
+        auto next_box = [&]() {                             // the other box of the two, read by the store before last
+            unsigned char *box = stg + box_at;
+            box_at ^= box_flip;
+            if (lane == 0) bulk_wait_read_1();
+            __syncwarp();
+            return box;
+        };
+        auto send_box = [&](const unsigned char *box, int x, int y, int z) {
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                if (OP != G_DW) tma_store_2d(&tmap_out, smem_u32(box), x, y);
+                else if (p.accumulate) tma_add_3d(&tmap_out, smem_u32(box), x, y, z);
+                else tma_store_3d(&tmap_out, smem_u32(box), x, y, z);
+                bulk_commit();
+            }
+        };
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
             const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
@@ -404,34 +434,57 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 }
             }
             if (!ok) break;
-            const int f = t.feature0 + (int)rank * 128 + quarter * 32 + lane;
+            const int f0 = t.feature0 + (int)rank * 128 + quarter * 32, f = f0 + lane;
+            // Output through boxes in shared memory where it is whole boxes (the map clips a store at 16 bytes, and at the last
+            // weight row, but not at the end of a group of lines).
+            const bool boxed = f0 + 32 <= p.features || p.features % (p.out_fp32 ? 4 : 8) == 0;
             // (accumulating: a group without rows adds nothing)
-            const int lines = f >= p.features || (OP == G_DW && p.accumulate && n_st == 0) ? 0 : t.line_count;
+            const int lines = f0 >= p.features || (OP == G_DW && p.accumulate && n_st == 0) ? 0 : t.line_count;
             const long long row0 = (OP == G_DW ? t.group * p.out_stride : 0ll) + (long long)t.line0 * p.ldo + f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int l0 = 64 * q + 32 * odd;
                 if (l0 >= lines) break;
                 const int n = min(32, lines - l0);
-                if (p.out_fp32) {
-                    float *dst = reinterpret_cast<float *>(p.out) + row0 + l0 * p.ldo;
-                    if (OP == G_DW && p.accumulate) {
+                if (boxed && (OP == G_DW || n == 32)) {
+                    if (p.out_fp32) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (OP == G_DW && 16 * h >= n) break;
+                            float *box = reinterpret_cast<float *>(next_box());
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) box[j * 32 + lane] = acc[q][16 * h + j];
+                            send_box(reinterpret_cast<unsigned char *>(box), f0, t.line0 + l0 + 16 * h, t.group);
+                        }
+                    } else {
+                        __nv_bfloat16 *box = reinterpret_cast<__nv_bfloat16 *>(next_box());
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) box[j * 32 + lane] = __float2bfloat16_rn(acc[q][j]);
+                        send_box(reinterpret_cast<unsigned char *>(box), f0, t.line0 + l0, t.group);
+                    }
+                } else if (f < p.features) {
+                    if (p.out_fp32) {
+                        float *dst = reinterpret_cast<float *>(p.out) + row0 + l0 * p.ldo;
+                        if (OP == G_DW && p.accumulate) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j < n) acc[q][j] += dst[j * p.ldo];
+                        }
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (j < n) acc[q][j] += dst[j * p.ldo];
+                            if (j < n) dst[j * p.ldo] = acc[q][j];
+                    } else {
+                        __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + row0 + l0 * p.ldo;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < n) dst[j * p.ldo] = __float2bfloat16_rn(acc[q][j]);
                     }
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < n) dst[j * p.ldo] = acc[q][j];
-                } else {
-                    __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + row0 + l0 * p.ldo;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < n) dst[j * p.ldo] = __float2bfloat16_rn(acc[q][j]);
                 }
+                __syncwarp();
             }
-            __syncwarp();
         }
+        if (lane == 0) bulk_wait_all();                     // this warp's stores are done
+        __syncwarp();
     }
 
     // teardown: nobody leaves while the other CTA may still read this one's memory or barriers
@@ -446,15 +499,15 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
 }
 
 template <int OP>
-static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const GroupedParams &p, long long most_tiles,
+static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const CUtensorMap &tmap_out, const GroupedParams &p, long long most_tiles,
                                   int sm_count, cudaStream_t st) {
     auto kern = mwu_gemm_grouped_kernel<OP>;
-    const size_t smem = 1024 + (size_t)G_STAGES * G_STAGE_BYTES + sizeof(GroupedSmem);
+    const size_t smem = 1024 + (size_t)G_STAGES * G_STAGE_BYTES + (size_t)G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const long long pairs = most_tiles < sm_count / 2 ? most_tiles : sm_count / 2;
     count_launch();
-    return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, maps_l, p);
+    return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, maps_l, tmap_out, p);
 }
 
 // box of 64 elements of the contiguous axis by `box_rows`, one group
@@ -466,6 +519,19 @@ static bool encode_bf16(EncodeTiledFn encode, CUtensorMap *tm, const void *ptr, 
     const cuuint32_t estr[3] = {1, 1, 1};
     return encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups ? 3 : 2, const_cast<void *>(ptr), gdim, gstride, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// an output box: 32 features of 16 lines of fp32, of 32 of bf16
+static bool encode_out(EncodeTiledFn encode, CUtensorMap *tm, void *ptr, bool fp32, int64_t features, int64_t lines, int64_t ld,
+                       int64_t groups, int64_t stride) {
+    const int64_t size = fp32 ? 4 : 2;
+    const cuuint64_t gdim[3] = {(cuuint64_t)features, (cuuint64_t)lines, (cuuint64_t)groups};
+    const cuuint64_t gstride[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(stride * size)};
+    const cuuint32_t box[3] = {32, (cuuint32_t)(fp32 ? 16 : 32), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return encode(tm, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups ? 3 : 2, ptr, gdim, gstride, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -504,7 +570,9 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? 128 : 64, groups, w_stride)) return MWU_ERR_CUDA;
     for (int b = 0; b < 3; ++b)
         if (!encode_bf16(encode, &maps_l.m[b], in, red, M, ldi, 128 >> b, 0, 0)) return MWU_ERR_CUDA;
-    return launch_grouped<OP>(tmap_f, maps_l, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+    CUtensorMap tmap_out;
+    if (!encode_out(encode, &tmap_out, out, out_dtype != 0, features, M, ldo, 0, 0)) return MWU_ERR_CUDA;
+    return launch_grouped<OP>(tmap_f, maps_l, tmap_out, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
 }
 
 }  // namespace gemm
@@ -557,5 +625,7 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     if (!encode_bf16(encode, &tmap_f, X, cols, m_rows, ldx, 64, 0, 0) || !encode_bf16(encode, &maps_l.m[0], dY, rows, m_rows, lddy, 64, 0, 0))
         return MWU_ERR_CUDA;
     maps_l.m[1] = maps_l.m[2] = maps_l.m[0];
-    return launch_grouped<G_DW>(tmap_f, maps_l, p, tiles, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
+    CUtensorMap tmap_out;
+    if (!encode_out(encode, &tmap_out, dW, dw_dtype != 0, cols, rows, lddw, groups, dw_stride)) return MWU_ERR_CUDA;
+    return launch_grouped<G_DW>(tmap_f, maps_l, tmap_out, p, tiles, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;
 }
