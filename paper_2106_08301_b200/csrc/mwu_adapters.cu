@@ -16,7 +16,7 @@
 //
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises MWU_DEV_TIMEOUT, waits for its copies in
 // flight, frees tensor memory and returns.
-#include "mwu_gemm_dev.cuh"
+#include "mwu_rows.cuh"
 
 namespace mwu {
 namespace gemm {
@@ -238,8 +238,7 @@ __device__ __forceinline__ unsigned cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
     return n;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 
 template <int R, bool F32>
 struct Few {
@@ -561,16 +560,6 @@ __device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap *map
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(unsigned taddr, unsigned (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
-}
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
 // place in a ring of slots: the slot and how often the ring has been gone round, for its parity
@@ -815,7 +804,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                     for (int q = 0; q < MINE / LD; ++q) {
                         unsigned v[LD];
                         const unsigned at = tmem_base + ((unsigned)(quarter * 32) << 16) + (use & 1u) * R + (unsigned)(col0 + q * LD);
-                        if constexpr (LD == 16) tmem_ld16(at, v);
+                        if constexpr (LD == 16) tmem_ld_16(at, v);
                         else tmem_ld32(at, v);
 #pragma unroll
                         for (int j = 0; j < LD; ++j) t[q * LD + j] += __uint_as_float(v[j]);

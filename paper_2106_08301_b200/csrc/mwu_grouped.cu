@@ -24,19 +24,19 @@
 // Roles per CTA (11 warps): warp 0 TMA producer, warp 1 tensor memory and (leader) MMAs, warps 2 to 9 epilogue (two per
 // 32-lane quarter, every other 32 lines), warp 10 zeroes foreign rows.  Every wait on an mbarrier is bounded; when one runs
 // out the kernel raises MWU_DEV_TIMEOUT, drains what it issued, frees tensor memory and returns.
-#include "mwu_gemm_dev.cuh"
+#include "mwu_rows.cuh"
 
 namespace mwu {
 namespace gemm {
 
 EncodeTiledFn get_encode_fn();          // mwu_gemm.cu
 
-constexpr int G_STAGES = 5;
+constexpr int G_RING = 180 * 1024;                   // bytes of stages
+constexpr int G_MOST_STAGES = 16;
 constexpr int G_EPI_WARPS = 8;
 constexpr int G_FIX_WARP = 2 + G_EPI_WARPS;
 constexpr int G_THREADS = 32 * (3 + G_EPI_WARPS);
-constexpr int G_SIDE = 128 * 128;                    // bytes of one operand of a stage in one CTA: 128 features or lines x 64
-constexpr int G_STAGE_BYTES = 2 * G_SIDE;
+constexpr int G_SIDE = 128 * 128;                    // bytes of 128 features or lines x 64 reduction steps
 constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 64 reduction steps
 constexpr int G_BOX = 2048;                          // of output: 32 features x 16 lines of fp32, x 32 of bf16; two to a warp
 constexpr int G_BAND = 8;                            // line tiles per band of the tile order
@@ -50,7 +50,9 @@ struct GroupedParams {
     long long ldo, out_stride;          // elements between output rows, between groups (weight gradient)
     int groups, M;
     int features, reduction, lines;     // reduction: of a product or input gradient; lines: of a weight gradient
-    int line_tile;                      // most lines of a tile
+    int line_tile;                      // most lines of a tile (a multiple of 32)
+    int feature_box;                    // product: weight rows of a box, as many as a CTA has of few features
+    int feature_side, stage_bytes, stages;      // of a stage: bytes of features, of all; stages in the ring
     int out_fp32, accumulate;
     unsigned *dev_status;
 };
@@ -58,10 +60,10 @@ struct GroupedParams {
 // The lines of a CTA's half tile as few boxes, whose issue takes as long as some of their transfer: 128 lines (from 97 on; what is
 // too many is never multiplied), 64 and 32, 64, or 32.  A weight gradient's boxes are 64 lines wide by 64 rows and take only m[0].
 struct LineMaps { CUtensorMap m[3]; };
-__device__ __forceinline__ int boxed_lines(int half) { return half > 96 ? 128 : (half + 31) & ~31; }
+__host__ __device__ __forceinline__ int boxed_lines(int half) { return half > 96 ? 128 : (half + 31) & ~31; }
 
 struct GroupedSmem {
-    unsigned long long full[G_STAGES], empty[G_STAGES], tail[G_STAGES], peer_fixed[G_STAGES], tfull[2], tempty[2], drain;
+    unsigned long long full[G_MOST_STAGES], empty[G_MOST_STAGES], tail[G_MOST_STAGES], peer_fixed[G_MOST_STAGES], tfull[2], tempty[2], drain;
     unsigned tmem_base;
     int abort, drain_abort;
     int n_live;                         // groups with rows
@@ -70,7 +72,7 @@ struct GroupedSmem {
     unsigned short live[MWU_MAX_GROUPS];
 };
 
-static_assert(1024 + G_STAGES * G_STAGE_BYTES + G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem) <= 232448, "grouped kernel: shared memory above 227 KB");
+static_assert(1024 + G_RING + G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem) <= 232448, "grouped kernel: shared memory above 227 KB");
 
 __device__ __forceinline__ void tma_load_3d_pair(unsigned dst, const CUtensorMap *map, unsigned bar_cluster, int x, int y, int z) {
     asm volatile(
@@ -114,6 +116,14 @@ __device__ __forceinline__ bool mbar_wait_cluster(unsigned bar, unsigned parity,
     }
 }
 
+// Bytes of features that the CTA with features f0 .. f0 + 127 of a tile loads for a stage: what lies wholly behind the last feature is
+// left out, since a lane without a feature may hold anything (a side as long as an adapter's rank: a quarter of the loads).
+template <int OP>
+__device__ __forceinline__ unsigned feature_bytes(const GroupedParams &p, int f0) {
+    if (f0 >= p.features) return 0u;
+    return OP == G_FORWARD ? (unsigned)p.feature_box * 128u : (f0 + 64 < p.features ? 2u : 1u) * (unsigned)G_SUB;
+}
+
 struct GroupedTile {
     int group, feature0, line0, line_count, line_pad;   // line0: row of X / dY, or weight row
     int red0, red_len;                                  // weight gradient: first row of the group and their number
@@ -125,7 +135,7 @@ template <int OP>
 __device__ __forceinline__ void grouped_tile(const GroupedParams &p, const GroupedSmem *sm, unsigned t, unsigned f_tiles, GroupedTile &o) {
     unsigned lt, n_lt, r;
     if (OP == G_DW) {
-        n_lt = (unsigned)(p.lines + 255) / 256;
+        n_lt = (unsigned)(p.lines + p.line_tile - 1) / (unsigned)p.line_tile;
         const unsigned per = n_lt * f_tiles, g = t / per;
         r = t - g * per;
         o.group = (int)g;
@@ -148,8 +158,8 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams &p, const Group
     lt = band * G_BAND + (rb - ft * wide);
     o.feature0 = (int)(ft * 256);
     if (OP == G_DW) {
-        o.line0 = (int)(lt * 256);
-        o.line_count = min(256, p.lines - o.line0);
+        o.line0 = (int)lt * p.line_tile;
+        o.line_count = min(p.line_tile, p.lines - o.line0);
     } else {
         const int begin = sm->offsets[o.group], len = sm->offsets[o.group + 1] - begin;
         // as many lines to every tile of the group, in whole 32s: never more than line_tile, and no tile is left empty
@@ -167,9 +177,8 @@ __global__ void __launch_bounds__(G_THREADS, 1)
 mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ LineMaps maps_l,
                         const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ GroupedParams p) {
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *sF = smem_raw + smem_pad_1024(smem_raw);
-    unsigned char *sL = sF + G_STAGES * G_SIDE;
-    unsigned char *boxes_out = sL + G_STAGES * G_SIDE;
+    unsigned char *ring = smem_raw + smem_pad_1024(smem_raw);
+    unsigned char *boxes_out = ring + G_RING;
     GroupedSmem *sm = reinterpret_cast<GroupedSmem *>(boxes_out + G_EPI_WARPS * 2 * G_BOX);
     volatile int *abort = &sm->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -178,7 +187,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     const unsigned f_tiles = (unsigned)(p.features + 255) / 256;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < G_STAGES; ++s) {
+        for (int s = 0; s < p.stages; ++s) {
             mbar_init(smem_u32(&sm->full[s]), 1);
             mbar_init(smem_u32(&sm->empty[s]), 1);
             mbar_init(smem_u32(&sm->tail[s]), 1);
@@ -236,7 +245,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     tc_fence_after();
     const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
     // (the host refuses sizes whose tile count could pass 2^31)
-    const unsigned total = bad ? 0u : OP == G_DW ? (unsigned)p.groups * f_tiles * ((unsigned)(p.lines + 255) / 256)
+    const unsigned total = bad ? 0u : OP == G_DW ? (unsigned)p.groups * f_tiles * ((unsigned)(p.lines + p.line_tile - 1) / (unsigned)p.line_tile)
                                                  : (unsigned)sm->cum[sm->n_live] * f_tiles;
     GroupedTile t;
 
@@ -250,33 +259,34 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
             const int n_st = (t.red_len + 63) / 64, half = t.line_pad / 2;
             const int f0 = t.feature0 + (int)rank * 128, l0 = t.line0 + (int)rank * half;
             const int boxes = (half + 63) / 64, boxed = boxed_lines(half);
-            const unsigned bytes = (unsigned)G_SIDE + (OP == G_DW ? (unsigned)boxes * G_SUB : (unsigned)boxed * 128u);
+            const unsigned line_bytes = OP == G_DW ? (unsigned)boxes * G_SUB : (unsigned)boxed * 128u;
+            const unsigned mine = feature_bytes<OP>(p, f0), pair_bytes = feature_bytes<OP>(p, t.feature0) + feature_bytes<OP>(p, t.feature0 + 128) + 2 * line_bytes;
             for (int ks = 0; ks < n_st; ++ks) {
                 if (!mbar_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort)) ok = false;
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 const bool tail = OP == G_DW && t.red_len - ks * 64 < 64 && ((t.red_len - ks * 64) & 15);
                 if (elect_one()) {
-                    const unsigned df = smem_u32(sF + stage * G_SIDE), dl = smem_u32(sL + stage * G_SIDE);
+                    const unsigned df = smem_u32(ring + stage * p.stage_bytes), dl = df + (unsigned)p.feature_side;
                     const int r0 = ks * 64;
                     if (tail) {
                         // foreign rows to zero: onto this CTA's own barrier, the fixing warp hands the stage on.  (A barrier to a
                         // slot: the next group's last stage may be under way before this one has landed.)
                         const unsigned bar = smem_u32(&sm->tail[stage]);
-                        mbar_expect_tx(bar, bytes);
-                        tma_load_2d(df, &tmap_f, bar, f0, t.red0 + r0);
-                        tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
+                        mbar_expect_tx(bar, mine + line_bytes);
+                        if (mine) tma_load_2d(df, &tmap_f, bar, f0, t.red0 + r0);
+                        if (mine > G_SUB) tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
                         for (int b = 0; b < boxes; ++b) tma_load_2d(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
                     } else {
                         const unsigned bar = mbar_addr_in_cta(smem_u32(&sm->full[stage]), 0);
-                        if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), 2 * bytes);
+                        if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), pair_bytes);
                         if (OP == G_FORWARD) {
-                            tma_load_3d_pair(df, &tmap_f, bar, r0, f0, t.group);
+                            if (mine) tma_load_3d_pair(df, &tmap_f, bar, r0, f0, t.group);
                         } else if (OP == G_DX) {
-                            tma_load_3d_pair(df, &tmap_f, bar, f0, r0, t.group);
-                            tma_load_3d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, r0, t.group);
+                            if (mine) tma_load_3d_pair(df, &tmap_f, bar, f0, r0, t.group);
+                            if (mine > G_SUB) tma_load_3d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, r0, t.group);
                         } else {
-                            tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
-                            tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
+                            if (mine) tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
+                            if (mine > G_SUB) tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
                         }
                         if (OP == G_DW) {
                             for (int b = 0; b < boxes; ++b) tma_load_2d_pair(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
@@ -289,15 +299,15 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 }
                 __syncwarp();
                 tails ^= (unsigned)tail << stage;
-                if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
             }
         }
         // a wait ran out: the loads in flight (of both CTAs, as far as they were issued) land before anybody leaves
         if (__any_sync(0xffffffffu, *abort)) {
             volatile int *drain_abort = &sm->drain_abort;
             if (rank == 0)
-                for (int s = 0; s < G_STAGES; ++s) mbar_wait(smem_u32(&sm->full[s]), s < stage ? phase : phase ^ 1u, drain_abort);
-            for (int s = 0; s < G_STAGES; ++s) mbar_wait(smem_u32(&sm->tail[s]), ((tails >> s) & 1u) ^ 1u, drain_abort);
+                for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->full[s]), s < stage ? phase : phase ^ 1u, drain_abort);
+            for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->tail[s]), ((tails >> s) & 1u) ^ 1u, drain_abort);
             __syncwarp();
         }
     } else if (warp == 1 && rank == 0) {
@@ -318,7 +328,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 for (int ks = c0; ks < c1; ++ks) {
                     if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort)) { ok = false; break; }
                     tc_fence_after();
-                    const unsigned af = smem_u32(sF + stage * G_SIDE), al = smem_u32(sL + stage * G_SIDE);
+                    const unsigned af = smem_u32(ring + stage * p.stage_bytes), al = af + (unsigned)p.feature_side;
                     const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
                     const unsigned long long ldesc = OP == G_DW ? make_desc_mn(al) : make_desc(al);
                     const int steps = min(4, (t.red_len - ks * 64 + 15) / 16);
@@ -330,7 +340,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                                            ldesc + (unsigned long long)(k4 * (OP == G_DW ? 128 : 2)), idesc, (ks > c0 || k4) ? 1u : 0u);
                         umma2_commit_both(smem_u32(&sm->empty[stage]));
                     }
-                    if (++stage == G_STAGES) { stage = 0; phase ^= 1u; }
+                    if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 if (elect_one()) umma2_commit_both(smem_u32(&sm->tfull[buf]));
@@ -352,15 +362,15 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 const unsigned n_st = (unsigned)(t.red_len + 63) / 64;
                 const int rem = t.red_len & 63;
                 if (rem & 15) {
-                    const unsigned stage = (pos + n_st - 1) % G_STAGES;
+                    const unsigned stage = (pos + n_st - 1) % (unsigned)p.stages;
                     ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort);
                     if (!ok) break;
                     // rows rem .. of the next multiple of 16, 128 bytes each, in the sub-tiles of either operand
                     const int rows = 16 - (rem & 15);
                     for (int i = lane; i < rows * 32; i += 32) {
-                        const int r = rem + (i >> 5), sub = (i >> 3) & 3, piece = i & 7;
-                        unsigned char *side = sub < 2 ? sF : sL;
-                        *reinterpret_cast<uint4 *>(side + stage * G_SIDE + (sub & 1) * G_SUB + r * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                        const int r = rem + (i >> 5), at = ((i >> 3) & 3) * G_SUB, piece = i & 7;      // at: the sub-tiles lie one behind the other
+                        if (at < p.stage_bytes)
+                            *reinterpret_cast<uint4 *>(ring + stage * p.stage_bytes + at + r * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async();
                     __syncwarp();
@@ -375,7 +385,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                     __syncwarp();
                     tails ^= 1u << stage;
                 }
-                pos = (pos + n_st) % G_STAGES;
+                pos = (pos + n_st) % (unsigned)p.stages;
             }
         }
     } else if (warp >= 2) {
@@ -502,7 +512,7 @@ template <int OP>
 static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const CUtensorMap &tmap_out, const GroupedParams &p, long long most_tiles,
                                   int sm_count, cudaStream_t st) {
     auto kern = mwu_gemm_grouped_kernel<OP>;
-    const size_t smem = 1024 + (size_t)G_STAGES * G_STAGE_BYTES + (size_t)G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem);
+    const size_t smem = 1024 + (size_t)G_RING + (size_t)G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const long long pairs = most_tiles < sm_count / 2 ? most_tiles : sm_count / 2;
@@ -535,6 +545,32 @@ static bool encode_out(EncodeTiledFn encode, CUtensorMap *tm, void *ptr, bool fp
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Most lines of a tile: what makes the shares of the CTA pairs take least, by an estimate in microseconds of a stage (its loads, which
+// the tensor cores wait for: 0.2 for 128 features and for 128 lines each) and of a tile's output.  `lines` in runs of which there are
+// `runs`, of unknown length: half a tile of each is taken to be lost.  (8192 rows 4096 -> 64: 128 lines 21 us, 256 lines 30;
+// 5003 rows of 12 groups 1096 -> 1416: 192 lines XX, 256 lines 34.)
+static int choose_line_tile(double lines, double runs, double copies, int64_t features, double stages, double out_us, int pairs) {
+    const double f_tiles = (double)((features + 255) / 256), per_feature = features >= 256 ? 0.2 : 0.2 * (double)((features + 63) / 64) / 4;
+    if (lines <= 24 * runs) return 64;                      // hardly a group has more: small stages, a long ring
+    double best = 1e30;
+    int tile = 256;
+    const int sizes[4] = {256, 192, 128, 64};
+    for (int t : sizes) {
+        const double tiles = f_tiles * copies * (lines / t + 0.5 * runs), rounds = tiles <= pairs ? 1.0 : tiles / pairs + 0.5;
+        const double us = rounds * (0.8 + stages * (0.05 + per_feature + 0.2 * t / 256) + out_us * t / 256);
+        if (us < 0.97 * best) { best = us; tile = t; }
+    }
+    return tile;
+}
+
+// Stages of what a CTA's share of the widest tile takes, as many as fit: loads are 2 us on their way, so a ring of few small stages
+// would wait for them (8192 rows 4096 -> 64: XX us with 11 stages of 16 KB, 27 with 5).
+static void lay_out_ring(GroupedParams &p, int feature_side, int line_side) {
+    p.feature_side = feature_side;
+    p.stage_bytes = feature_side + line_side;
+    p.stages = G_RING / p.stage_bytes < G_MOST_STAGES ? G_RING / p.stage_bytes : G_MOST_STAGES;
+}
+
 // Y = X . W^T and dX = dY . W: `red` / `features` = cols / rows of the weights, or rows / cols
 template <int OP>
 static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride, const int32_t *offsets,
@@ -554,20 +590,23 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     p.offsets = offsets;
     p.out = out; p.ldo = ldo; p.out_fp32 = out_dtype;
     p.groups = (int)groups; p.M = (int)M; p.features = (int)features; p.reduction = (int)red;
-    p.line_tile = 256;
+    p.feature_box = features <= 32 ? 32 : features <= 64 ? 64 : 128;
     p.dev_status = dev_status;
     const int64_t f_tiles = (features + 255) / 256;
-    const int64_t most = (M / p.line_tile + (M < groups ? M : groups)) * f_tiles;
-    if (most >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
+    if ((M / 32 + (M < groups ? M : groups)) * f_tiles >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
     int sm_count = 0;
     const int rc = check_device(&sm_count);
     if (rc != MWU_OK) return rc;
     if (M == 0) return MWU_OK;
+    const int64_t runs = M < groups ? M : groups;
+    p.line_tile = choose_line_tile((double)M, (double)runs, 1.0, features, (double)((red + 63) / 64), out_dtype ? 1.6 : 1.2, sm_count / 2);
+    const int64_t most = (M / p.line_tile + runs) * f_tiles;
+    lay_out_ring(p, features <= 32 && OP == G_FORWARD ? 4096 : features <= 64 ? G_SUB : G_SIDE, boxed_lines(p.line_tile / 2) * 128);
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
     CUtensorMap tmap_f;
     LineMaps maps_l;
-    if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? 128 : 64, groups, w_stride)) return MWU_ERR_CUDA;
+    if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? p.feature_box : 64, groups, w_stride)) return MWU_ERR_CUDA;
     for (int b = 0; b < 3; ++b)
         if (!encode_bf16(encode, &maps_l.m[b], in, red, M, ldi, 128 >> b, 0, 0)) return MWU_ERR_CUDA;
     CUtensorMap tmap_out;
@@ -610,13 +649,14 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     p.offsets = offsets;
     p.out = dW; p.ldo = lddw; p.out_stride = dw_stride; p.out_fp32 = dw_dtype; p.accumulate = accumulate;
     p.groups = (int)groups; p.M = (int)M; p.features = (int)cols; p.lines = (int)rows;
-    p.line_tile = 256;
     p.dev_status = dev_status;
-    const int64_t tiles = groups * ((rows + 255) / 256) * ((cols + 255) / 256);
-    if (tiles >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
+    if (groups * ((rows + 63) / 64) * ((cols + 255) / 256) >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
     int sm_count = 0;
     const int rc = check_device(&sm_count);
     if (rc != MWU_OK) return rc;
+    p.line_tile = choose_line_tile((double)rows, 1.0, (double)groups, cols, (double)M / (64.0 * groups), dw_dtype ? 3.2 : 1.6, sm_count / 2);
+    const int64_t tiles = groups * ((rows + p.line_tile - 1) / p.line_tile) * ((cols + 255) / 256);
+    lay_out_ring(p, cols <= 64 ? G_SUB : G_SIDE, (p.line_tile / 2 + 63) / 64 * G_SUB);
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
     CUtensorMap tmap_f;
