@@ -181,7 +181,8 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     unsigned char *boxes_out = ring + G_RING;
     GroupedSmem *sm = reinterpret_cast<GroupedSmem *>(boxes_out + G_EPI_WARPS * 2 * G_BOX);
     volatile int *abort = &sm->abort;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // (the same in all lanes, and known to be: what hangs on it then lives in uniform registers, which MMAs and copies take their operands from)
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const unsigned rank = cluster_rank();               // 0: leader (issues the MMAs), 1: peer
     const unsigned pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
     const unsigned f_tiles = (unsigned)(p.features + 255) / 256;
@@ -243,7 +244,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     __syncthreads();
     cluster_sync_all();                                 // both CTAs' barriers exist before any remote arrive
     tc_fence_after();
-    const unsigned tmem_base = *reinterpret_cast<volatile unsigned *>(&sm->tmem_base);
+    const unsigned tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile unsigned *>(&sm->tmem_base), 0);
     // (the host refuses sizes whose tile count could pass 2^31)
     const unsigned total = bad ? 0u : OP == G_DW ? (unsigned)p.groups * f_tiles * ((unsigned)(p.lines + p.line_tile - 1) / (unsigned)p.line_tile)
                                                  : (unsigned)sm->cum[sm->n_live] * f_tiles;
@@ -317,21 +318,22 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         bool ok = true;
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
-            const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
-            const unsigned idesc = make_idesc_pair(t.line_pad) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
+            const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_st = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
+            const unsigned idesc = make_idesc_pair(__shfl_sync(0xffffffffu, t.line_pad, 0)) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
             for (int c0 = 0; ok && c0 < n_st; c0 += chunk, ++use) {
                 const unsigned buf = use & 1u;
-                if (!mbar_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort)) ok = false;
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                ok = warp_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort);
+                if (!ok) break;
                 tc_fence_after();
                 const int c1 = min(n_st, c0 + chunk);
                 for (int ks = c0; ks < c1; ++ks) {
-                    if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort)) { ok = false; break; }
+                    ok = warp_wait_spin(smem_u32(&sm->full[stage]), phase, abort);
+                    if (!ok) break;
                     tc_fence_after();
-                    const unsigned af = smem_u32(ring + stage * p.stage_bytes), al = af + (unsigned)p.feature_side;
+                    const unsigned af = smem_u32(ring) + (unsigned)(stage * p.stage_bytes), al = af + (unsigned)p.feature_side;
                     const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
                     const unsigned long long ldesc = OP == G_DW ? make_desc_mn(al) : make_desc(al);
-                    const int steps = min(4, (t.red_len - ks * 64 + 15) / 16);
+                    const int steps = min(4, (red_len - ks * 64 + 15) / 16);
                     if (elect_one()) {
 #pragma unroll
                         for (int k4 = 0; k4 < 4; ++k4)
@@ -340,9 +342,10 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                                            ldesc + (unsigned long long)(k4 * (OP == G_DW ? 128 : 2)), idesc, (ks > c0 || k4) ? 1u : 0u);
                         umma2_commit_both(smem_u32(&sm->empty[stage]));
                     }
+                    __syncwarp();
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                if (!ok) break;
                 if (elect_one()) umma2_commit_both(smem_u32(&sm->tfull[buf]));
                 __syncwarp();
             }
