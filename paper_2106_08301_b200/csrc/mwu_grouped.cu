@@ -52,7 +52,8 @@ struct GroupedParams {
     int features, reduction, lines;     // reduction: of a product or input gradient; lines: of a weight gradient
     int line_tile;                      // most lines of a tile (a multiple of 32)
     int feature_box;                    // product: weight rows of a box, as many as a CTA has of few features
-    int feature_side, stage_bytes, stages;      // of a stage: bytes of features, of all; stages in the ring
+    int feature_side, block_bytes;      // of 64 reduction steps: bytes of features, of all
+    int blocks, stages;                 // blocks of a stage, stages of the ring
     int out_fp32, accumulate;
     unsigned *dev_status;
 };
@@ -172,7 +173,7 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams &p, const Group
     o.line_pad = (o.line_count + 31) & ~31;
 }
 
-template <int OP>
+template <int OP, int BL>
 __global__ void __launch_bounds__(G_THREADS, 1)
 mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ LineMaps maps_l,
                         const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ GroupedParams p) {
@@ -257,44 +258,52 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         bool ok = true;
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
-            const int n_st = (t.red_len + 63) / 64, half = t.line_pad / 2;
+            const int n_blk = (t.red_len + 63) / 64, half = t.line_pad / 2;
             const int f0 = t.feature0 + (int)rank * 128, l0 = t.line0 + (int)rank * half;
             const int boxes = (half + 63) / 64, boxed = boxed_lines(half);
             const unsigned line_bytes = OP == G_DW ? (unsigned)boxes * G_SUB : (unsigned)boxed * 128u;
             const unsigned mine = feature_bytes<OP>(p, f0), pair_bytes = feature_bytes<OP>(p, t.feature0) + feature_bytes<OP>(p, t.feature0 + 128) + 2 * line_bytes;
-            for (int ks = 0; ks < n_st; ++ks) {
-                if (!mbar_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort)) ok = false;
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const bool tail = OP == G_DW && t.red_len - ks * 64 < 64 && ((t.red_len - ks * 64) & 15);
+            for (int b0 = 0; b0 < n_blk; b0 += BL) {
+                ok = warp_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort);
+                if (!ok) break;
+                const int nb = min(BL, n_blk - b0), last = t.red_len - (b0 + nb - 1) * 64;     // reduction steps from the last block on
+                const bool tail = OP == G_DW && last < 64 && (last & 15);
                 if (elect_one()) {
-                    const unsigned df = smem_u32(ring + stage * p.stage_bytes), dl = df + (unsigned)p.feature_side;
-                    const int r0 = ks * 64;
+                    unsigned df = smem_u32(ring) + (unsigned)(stage * BL * p.block_bytes);
                     if (tail) {
                         // foreign rows to zero: onto this CTA's own barrier, the fixing warp hands the stage on.  (A barrier to a
                         // slot: the next group's last stage may be under way before this one has landed.)
                         const unsigned bar = smem_u32(&sm->tail[stage]);
-                        mbar_expect_tx(bar, mine + line_bytes);
-                        if (mine) tma_load_2d(df, &tmap_f, bar, f0, t.red0 + r0);
-                        if (mine > G_SUB) tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
-                        for (int b = 0; b < boxes; ++b) tma_load_2d(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
+                        mbar_expect_tx(bar, (unsigned)nb * (mine + line_bytes));
+                        for (int b = 0; b < nb; ++b, df += (unsigned)p.block_bytes) {
+                            const unsigned dl = df + (unsigned)p.feature_side;
+                            const int row = t.red0 + (b0 + b) * 64;
+                            if (mine) tma_load_2d(df, &tmap_f, bar, f0, row);
+                            if (mine > G_SUB) tma_load_2d(df + G_SUB, &tmap_f, bar, f0 + 64, row);
+                            for (int j = 0; j < boxes; ++j) tma_load_2d(dl + j * G_SUB, &maps_l.m[0], bar, l0 + 64 * j, row);
+                        }
                     } else {
                         const unsigned bar = mbar_addr_in_cta(smem_u32(&sm->full[stage]), 0);
-                        if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), pair_bytes);
-                        if (OP == G_FORWARD) {
-                            if (mine) tma_load_3d_pair(df, &tmap_f, bar, r0, f0, t.group);
-                        } else if (OP == G_DX) {
-                            if (mine) tma_load_3d_pair(df, &tmap_f, bar, f0, r0, t.group);
-                            if (mine > G_SUB) tma_load_3d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, r0, t.group);
-                        } else {
-                            if (mine) tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
-                            if (mine > G_SUB) tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
-                        }
-                        if (OP == G_DW) {
-                            for (int b = 0; b < boxes; ++b) tma_load_2d_pair(dl + b * G_SUB, &maps_l.m[0], bar, l0 + 64 * b, t.red0 + r0);
-                        } else {
-                            if (boxed == 128) tma_load_2d_pair(dl, &maps_l.m[0], bar, r0, l0);
-                            else if (boxed & 64) tma_load_2d_pair(dl, &maps_l.m[1], bar, r0, l0);
-                            if (boxed & 32) tma_load_2d_pair(dl + (boxed & 64) * 128, &maps_l.m[2], bar, r0, l0 + (boxed & 64));
+                        if (rank == 0) mbar_expect_tx(smem_u32(&sm->full[stage]), (unsigned)nb * pair_bytes);
+                        for (int b = 0; b < nb; ++b, df += (unsigned)p.block_bytes) {
+                            const unsigned dl = df + (unsigned)p.feature_side;
+                            const int r0 = (b0 + b) * 64;
+                            if (OP == G_FORWARD) {
+                                if (mine) tma_load_3d_pair(df, &tmap_f, bar, r0, f0, t.group);
+                            } else if (OP == G_DX) {
+                                if (mine) tma_load_3d_pair(df, &tmap_f, bar, f0, r0, t.group);
+                                if (mine > G_SUB) tma_load_3d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, r0, t.group);
+                            } else {
+                                if (mine) tma_load_2d_pair(df, &tmap_f, bar, f0, t.red0 + r0);
+                                if (mine > G_SUB) tma_load_2d_pair(df + G_SUB, &tmap_f, bar, f0 + 64, t.red0 + r0);
+                            }
+                            if (OP == G_DW) {
+                                for (int j = 0; j < boxes; ++j) tma_load_2d_pair(dl + j * G_SUB, &maps_l.m[0], bar, l0 + 64 * j, t.red0 + r0);
+                            } else {
+                                if (boxed == 128) tma_load_2d_pair(dl, &maps_l.m[0], bar, r0, l0);
+                                else if (boxed & 64) tma_load_2d_pair(dl, &maps_l.m[1], bar, r0, l0);
+                                if (boxed & 32) tma_load_2d_pair(dl + (boxed & 64) * 128, &maps_l.m[2], bar, r0, l0 + (boxed & 64));
+                            }
                         }
                     }
                 }
@@ -318,28 +327,32 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         bool ok = true;
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
-            const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_st = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
+            const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_blk = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_blk;
             const unsigned idesc = make_idesc_pair(__shfl_sync(0xffffffffu, t.line_pad, 0)) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
-            for (int c0 = 0; ok && c0 < n_st; c0 += chunk, ++use) {
+            for (int c0 = 0; ok && c0 < n_blk; c0 += chunk, ++use) {
                 const unsigned buf = use & 1u;
                 ok = warp_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort);
                 if (!ok) break;
                 tc_fence_after();
-                const int c1 = min(n_st, c0 + chunk);
-                for (int ks = c0; ks < c1; ++ks) {
+                const int c1 = min(n_blk, c0 + chunk);
+                for (int b0 = c0; b0 < c1; b0 += BL) {
                     ok = warp_wait_spin(smem_u32(&sm->full[stage]), phase, abort);
                     if (!ok) break;
                     tc_fence_after();
-                    const unsigned af = smem_u32(ring) + (unsigned)(stage * p.stage_bytes), al = af + (unsigned)p.feature_side;
-                    const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
-                    const unsigned long long ldesc = OP == G_DW ? make_desc_mn(al) : make_desc(al);
-                    const int steps = min(4, (red_len - ks * 64 + 15) / 16);
+                    const int nb = min(BL, n_blk - b0);
+                    unsigned af = smem_u32(ring) + (unsigned)(stage * BL * p.block_bytes);
                     if (elect_one()) {
+                        for (int b = b0; b < b0 + nb; ++b, af += (unsigned)p.block_bytes) {
+                            const unsigned al = af + (unsigned)p.feature_side;
+                            const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
+                            const unsigned long long ldesc = OP == G_DW ? make_desc_mn(al) : make_desc(al);
+                            const int steps = min(4, (red_len - b * 64 + 15) / 16);
 #pragma unroll
-                        for (int k4 = 0; k4 < 4; ++k4)
-                            if (k4 < steps)                 // 16 products on: 32 bytes K-major, two groups of 8 rows MN-major
-                                umma2_bf16(tmem_base + buf * 256u, fdesc + (unsigned long long)(k4 * (OP == G_FORWARD ? 2 : 128)),
-                                           ldesc + (unsigned long long)(k4 * (OP == G_DW ? 128 : 2)), idesc, (ks > c0 || k4) ? 1u : 0u);
+                            for (int k4 = 0; k4 < 4; ++k4)
+                                if (k4 < steps)             // 16 products on: 32 bytes K-major, two groups of 8 rows MN-major
+                                    umma2_bf16(tmem_base + buf * 256u, fdesc + (unsigned long long)(k4 * (OP == G_FORWARD ? 2 : 128)),
+                                               ldesc + (unsigned long long)(k4 * (OP == G_DW ? 128 : 2)), idesc, (b > c0 || k4) ? 1u : 0u);
+                        }
                         umma2_commit_both(smem_u32(&sm->empty[stage]));
                     }
                     __syncwarp();
@@ -362,7 +375,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
             bool ok = true;
             for (unsigned k = pair; ok && k < total; k += n_pairs) {
                 grouped_tile<OP>(p, sm, k, f_tiles, t);
-                const unsigned n_st = (unsigned)(t.red_len + 63) / 64;
+                const unsigned n_blk = (unsigned)(t.red_len + 63) / 64, n_st = (n_blk + (unsigned)BL - 1) / (unsigned)BL;
                 const int rem = t.red_len & 63;
                 if (rem & 15) {
                     const unsigned stage = (pos + n_st - 1) % (unsigned)p.stages;
@@ -370,10 +383,10 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                     if (!ok) break;
                     // rows rem .. of the next multiple of 16, 128 bytes each, in the sub-tiles of either operand
                     const int rows = 16 - (rem & 15);
+                    unsigned char *block = ring + (stage * (unsigned)BL + (n_blk - 1) % (unsigned)BL) * (unsigned)p.block_bytes;
                     for (int i = lane; i < rows * 32; i += 32) {
                         const int r = rem + (i >> 5), at = ((i >> 3) & 3) * G_SUB, piece = i & 7;      // at: the sub-tiles lie one behind the other
-                        if (at < p.stage_bytes)
-                            *reinterpret_cast<uint4 *>(ring + stage * p.stage_bytes + at + r * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                        if (at < p.block_bytes) *reinterpret_cast<uint4 *>(block + at + r * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async();
                     __syncwarp();
@@ -511,16 +524,24 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     }
 }
 
-template <int OP>
-static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const CUtensorMap &tmap_out, const GroupedParams &p, long long most_tiles,
+template <int OP, int BL>
+static cudaError_t launch_grouped_bl(const CUtensorMap &tmap_f, const LineMaps &maps_l, const CUtensorMap &tmap_out, const GroupedParams &p, long long most_tiles,
                                   int sm_count, cudaStream_t st) {
-    auto kern = mwu_gemm_grouped_kernel<OP>;
+    auto kern = mwu_gemm_grouped_kernel<OP, BL>;
     const size_t smem = 1024 + (size_t)G_RING + (size_t)G_EPI_WARPS * 2 * G_BOX + sizeof(GroupedSmem);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const long long pairs = most_tiles < sm_count / 2 ? most_tiles : sm_count / 2;
     count_launch();
     return launch_chained(kern, dim3((unsigned)(2 * pairs)), dim3(G_THREADS), smem, st, 2, tmap_f, maps_l, tmap_out, p);
+}
+
+template <int OP>
+static cudaError_t launch_grouped(const CUtensorMap &tmap_f, const LineMaps &maps_l, const CUtensorMap &tmap_out, const GroupedParams &p,
+                                  long long most_tiles, int sm_count, cudaStream_t st) {
+    if constexpr (OP != G_DW)
+        if (p.blocks == 2) return launch_grouped_bl<OP, 2>(tmap_f, maps_l, tmap_out, p, most_tiles, sm_count, st);
+    return launch_grouped_bl<OP, 1>(tmap_f, maps_l, tmap_out, p, most_tiles, sm_count, st);
 }
 
 // box of 64 elements of the contiguous axis by `box_rows`, one group
@@ -566,12 +587,16 @@ static int choose_line_tile(double lines, double runs, double copies, int64_t fe
     return tile;
 }
 
-// Stages of what a CTA's share of the widest tile takes, as many as fit: loads are 2 us on their way, so a ring of few small stages
-// would wait for them (8192 rows 4096 -> 64: XX us with 11 stages of 16 KB, 27 with 5).
-static void lay_out_ring(GroupedParams &p, int feature_side, int line_side) {
+// Stages of what a CTA's share of the widest tile takes, as many as fit: loads are 2 us on their way.  A stage costs 0.27 us whatever
+// it holds (the commits that hand its slot back to both CTAs follow one another at that pace), so small blocks go two to a stage
+// (8192 rows 4096 -> 64: 23.5 us, 26 with one; 2 rows of 1024 x 1024: 9.2, 10.0), but not where three stages would be left (weight
+// gradients of a side of 64: 28.7, 25.6 with one), and in a kernel of its own (full tiles: 2 to 6 % slower with the loop).
+static void lay_out_ring(GroupedParams &p, int feature_side, int line_side, bool pairs) {
     p.feature_side = feature_side;
-    p.stage_bytes = feature_side + line_side;
-    p.stages = G_RING / p.stage_bytes < G_MOST_STAGES ? G_RING / p.stage_bytes : G_MOST_STAGES;
+    p.block_bytes = feature_side + line_side;
+    p.blocks = pairs && p.block_bytes <= 20 * 1024 ? 2 : 1;
+    const int fit = G_RING / (p.blocks * p.block_bytes);
+    p.stages = fit < G_MOST_STAGES ? fit : G_MOST_STAGES;
 }
 
 // Y = X . W^T and dX = dY . W: `red` / `features` = cols / rows of the weights, or rows / cols
@@ -604,7 +629,7 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     const int64_t runs = M < groups ? M : groups;
     p.line_tile = choose_line_tile((double)M, (double)runs, 1.0, features, (double)((red + 63) / 64), out_dtype ? 1.6 : 1.2, sm_count / 2);
     const int64_t most = (M / p.line_tile + runs) * f_tiles;
-    lay_out_ring(p, features <= 32 && OP == G_FORWARD ? 4096 : features <= 64 ? G_SUB : G_SIDE, boxed_lines(p.line_tile / 2) * 128);
+    lay_out_ring(p, features <= 32 && OP == G_FORWARD ? 4096 : features <= 64 ? G_SUB : G_SIDE, boxed_lines(p.line_tile / 2) * 128, true);
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
     CUtensorMap tmap_f;
@@ -659,7 +684,7 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     if (rc != MWU_OK) return rc;
     p.line_tile = choose_line_tile((double)rows, 1.0, (double)groups, cols, (double)M / (64.0 * groups), dw_dtype ? 3.2 : 1.6, sm_count / 2);
     const int64_t tiles = groups * ((rows + p.line_tile - 1) / p.line_tile) * ((cols + 255) / 256);
-    lay_out_ring(p, cols <= 64 ? G_SUB : G_SIDE, (p.line_tile / 2 + 63) / 64 * G_SUB);
+    lay_out_ring(p, cols <= 64 ? G_SUB : G_SIDE, (p.line_tile / 2 + 63) / 64 * G_SUB, false);
     EncodeTiledFn encode = get_encode_fn();
     if (!encode) return MWU_ERR_CUDA;
     CUtensorMap tmap_f;
