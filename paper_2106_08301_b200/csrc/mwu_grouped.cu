@@ -336,8 +336,8 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 tc_fence_after();
                 const int c1 = min(n_blk, c0 + chunk);
                 for (int b0 = c0; b0 < c1; b0 += BL) {
-                    ok = warp_wait_spin(smem_u32(&sm->full[stage]), phase, abort);
-                    if (!ok) break;
+                    // (no vote and no warp barrier: every lane looks at the same barriers and decides alike)
+                    if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort)) { ok = false; break; }
                     tc_fence_after();
                     const int nb = min(BL, n_blk - b0);
                     unsigned af = smem_u32(ring) + (unsigned)(stage * BL * p.block_bytes);
@@ -355,9 +355,9 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                         }
                         umma2_commit_both(smem_u32(&sm->empty[stage]));
                     }
-                    __syncwarp();
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (elect_one()) umma2_commit_both(smem_u32(&sm->tfull[buf]));
                 __syncwarp();
