@@ -142,6 +142,19 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _operands(device: int, *tensors):
+    """Addresses of (tensor or None, type) pairs, each of that type, contiguous and on `device`: a kernel reads what it is given as its own type."""
+    out = []
+    for t, dtype in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype != dtype or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"contiguous {dtype} tensors of the current device only: got {t.dtype} on {t.device}")
+        out.append(t.data_ptr())
+    return out
+
+
 def status_string(status: int) -> str:
     return lib().mwu_status_string(int(status)).decode()
 
@@ -290,10 +303,15 @@ def mwu_conv_dense(rows, Wd, ldw, X, n, c, h, w, kh, kw, stride, pad, Y, y_dtype
     return rc
 
 
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
 def mwu_gemm_grouped(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, Y, ldy, y_dtype, dev_status, stream=None,
                      check=True) -> int:
-    rc = lib().mwu_gemm_grouped(int(groups), int(rows), int(cols), _ptr(Wd), int(ldw), int(w_stride), _ptr(offsets), _ptr(X),
-                                int(M), int(ldx), _ptr(Y), int(ldy), int(y_dtype), _ptr(dev_status), _stream(stream))
+    """Y[m] = X[m] W_g^T for the rows m of every group g."""
+    w, o, x, y, st = _operands(torch.cuda.current_device(), (Wd, _BF16), (offsets, _I32), (X, _BF16), (Y, _F32 if y_dtype else _BF16),
+                               (dev_status, _I32))
+    rc = lib().mwu_gemm_grouped(groups, rows, cols, w, ldw, w_stride, o, x, M, ldx, y, ldy, y_dtype, st, _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped")
     return rc
@@ -301,9 +319,10 @@ def mwu_gemm_grouped(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, 
 
 def mwu_gemm_grouped_dx(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, lddy, dX, lddx, dx_dtype, dev_status,
                         stream=None, check=True) -> int:
-    rc = lib().mwu_gemm_grouped_dx(int(groups), int(rows), int(cols), _ptr(Wd), int(ldw), int(w_stride), _ptr(offsets),
-                                   _ptr(dY), int(M), int(lddy), _ptr(dX), int(lddx), int(dx_dtype), _ptr(dev_status),
-                                   _stream(stream))
+    """dX[m] = dY[m] W_g for the rows m of every group g."""
+    w, o, d, x, st = _operands(torch.cuda.current_device(), (Wd, _BF16), (offsets, _I32), (dY, _BF16), (dX, _F32 if dx_dtype else _BF16),
+                               (dev_status, _I32))
+    rc = lib().mwu_gemm_grouped_dx(groups, rows, cols, w, ldw, w_stride, o, d, M, lddy, x, lddx, dx_dtype, st, _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped_dx")
     return rc
@@ -311,9 +330,11 @@ def mwu_gemm_grouped_dx(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, l
 
 def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, lddw, dw_stride, dw_dtype, accumulate,
                         dev_status, stream=None, check=True) -> int:
-    rc = lib().mwu_gemm_grouped_dw(int(groups), int(rows), int(cols), _ptr(offsets), _ptr(dY), int(M), int(lddy), _ptr(X),
-                                   int(ldx), _ptr(dW), int(lddw), int(dw_stride), int(dw_dtype), int(accumulate),
-                                   _ptr(dev_status), _stream(stream))
+    """dW_g = dY_g^T X_g (accumulate: added to dW_g)."""
+    o, d, x, w, st = _operands(torch.cuda.current_device(), (offsets, _I32), (dY, _BF16), (X, _BF16), (dW, _F32 if dw_dtype else _BF16),
+                               (dev_status, _I32))
+    rc = lib().mwu_gemm_grouped_dw(groups, rows, cols, o, d, M, lddy, x, ldx, w, lddw, dw_stride, dw_dtype, accumulate, st,
+                                   _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped_dw")
     return rc
@@ -321,9 +342,12 @@ def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, ld
 
 def mwu_adapters_add(adapters, rank, rows, cols, A, lda, a_stride, Bm, ldb, b_stride, scale, segments, offsets, which, X, M,
                      ldx, Y0, Y, ldy, y_dtype, dev_status, stream=None, check=True) -> int:
-    rc = lib().mwu_adapters_add(int(adapters), int(rank), int(rows), int(cols), _ptr(A), int(lda), int(a_stride), _ptr(Bm),
-                                int(ldb), int(b_stride), _ptr(scale), int(segments), _ptr(offsets), _ptr(which), _ptr(X), int(M),
-                                int(ldx), _ptr(Y0), _ptr(Y), int(ldy), int(y_dtype), _ptr(dev_status), _stream(stream))
+    """Y = Y0 + scale (X A^T) B^T for segments of rows with an adapter each (Y0 None: zeros; Y itself: in place)."""
+    out = _F32 if y_dtype else _BF16
+    a, b, sc, o, w, x, y0, y, st = _operands(torch.cuda.current_device(), (A, _BF16), (Bm, _BF16), (scale, _F32), (offsets, _I32),
+                                             (which, _I32), (X, _BF16), (Y0, out), (Y, out), (dev_status, _I32))
+    rc = lib().mwu_adapters_add(adapters, rank, rows, cols, a, lda, a_stride, b, ldb, b_stride, sc, segments, o, w, x, M, ldx, y0, y,
+                                ldy, y_dtype, st, _stream(stream))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_adapters_add")
     return rc

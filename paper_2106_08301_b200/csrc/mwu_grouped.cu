@@ -571,8 +571,8 @@ static bool encode_out(EncodeTiledFn encode, CUtensorMap *tm, void *ptr, bool fp
 
 // Most lines of a tile: what makes the shares of the CTA pairs take least, by an estimate in microseconds of a stage (its loads, which
 // the tensor cores wait for: 0.2 for 128 features and for 128 lines each) and of a tile's output.  `lines` in runs of which there are
-// `runs`, of unknown length: half a tile of each is taken to be lost.  (8192 rows 4096 -> 64: 128 lines 21 us, 256 lines 30;
-// 5003 rows of 12 groups 1096 -> 1416: 192 lines XX, 256 lines 34.)
+// `runs`, of unknown length: half a tile of each is taken to be lost.  (8192 rows of 4 groups, 4096 -> 64: 27 us with 128 lines, 31 with 256,
+// both with five stages; 256 rows of 64 groups, 4096 -> 2048: 170 with 64, whose ring is longer, 179 with 256.)
 static int choose_line_tile(double lines, double runs, double copies, int64_t features, double stages, double out_us, int pairs) {
     const double f_tiles = (double)((features + 255) / 256), per_feature = features >= 256 ? 0.2 : 0.2 * (double)((features + 63) / 64) / 4;
     if (lines <= 24 * runs) return 64;                      // hardly a group has more: small stages, a long ring

@@ -6,6 +6,9 @@ sum |x| |a| as for the grouped products, and cols / 512 + 8 roundings of 2^-24 w
 product as bf16 terms that leave out 2^-17 of it (two) or 2^-25 (three), which the next product adds up over rank / 16 steps a
 term, within 2^-22 of the running magnitude each.  Y adds one rounding of 2^-24, and half a step of bf16, 2^-8, where it is bf16.
 """
+import math
+import random
+
 import pytest
 import torch
 
@@ -119,6 +122,37 @@ def test_against_the_formula(lengths, adapters, rank, rows, cols, fp32):
         b.run(None, V)                                      # nothing to add to
         b.check(V, None, before)
         assert int(b.st.item()) == 0
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_drawn_batches(seed):
+    r = random.Random(seed)
+    log = lambda lo, hi: int(round(math.exp(r.uniform(math.log(lo), math.log(hi)))))
+    lengths = [1] * r.choice([0, log(1, 90)]) + [log(2, 1500) for _ in range(r.choice([0, 1, 3, 6]))] + [0] * r.choice([0, 2])
+    r.shuffle(lengths)
+    lengths = lengths or [1]
+    adapters, rank, rows, cols = log(1, 20), r.choice([1, 7, 16, 31, 64, 65, 128, r.randrange(1, 129)]), log(1, 1100), log(1, 1500)
+    b = Batch(lengths, [r.randrange(-1, adapters) for _ in lengths], adapters, rank, rows, cols, r.randrange(2), seed=seed, first=r.choice([0, 3]),
+              behind=r.choice([0, 5]), pad=r.random() < 0.7, with_scale=r.random() < 0.7)
+    before = torch.full_like(b.Y0, 777.0)
+    Y = before.clone()
+    b.run(b.Y0, Y)
+    torch.cuda.synchronize()
+    assert int(b.st.item()) == 0
+    b.check(Y, b.Y0, before)
+
+
+def test_rows_of_one_adapter_all_over_the_batch():
+    """A small batch is worked on adapter by adapter: many rows of one, in segments that lie apart, empty ones between."""
+    lengths = [1, 0, 3, 1, 1, 0, 0, 20, 1, 1, 2, 1, 17, 1, 1, 1, 40, 1] + [1] * 60
+    which = [(s * s) % 3 - 1 if s < 18 else 1 for s in range(len(lengths))]
+    for fp32 in (0, 1):
+        b = Batch(lengths, which, 2, 16, 264, 520, fp32)
+        Z = b.Y0.clone()
+        b.run(Z, Z)
+        torch.cuda.synchronize()
+        assert int(b.st.item()) == 0
+        b.check(Z, b.Y0, b.Y0)
 
 
 def test_without_scales_and_without_padding():

@@ -6,6 +6,7 @@ with K the length of a piece (512) where the result is fp32, and the pieces are 
 A bf16 result adds half a step of it, 2^-8.
 """
 import math
+import random
 
 import pytest
 import torch
@@ -142,6 +143,38 @@ def test_weight_gradient(lengths, rows, cols, mode):
             assert torch.equal(dW[g, :rows, :cols], before[g, :rows, :cols] if mode == "accumulate" else torch.zeros_like(before[g, :rows, :cols]))
         else:
             check(dW[g, :rows, :cols], ref, mag, lengths[g], fp32)
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_drawn_sizes(seed):
+    """Sizes between the listed ones: every height of tile, sides as long as a rank, few and many rows to a group."""
+    r = random.Random(seed)
+    log = lambda lo, hi: int(round(math.exp(r.uniform(math.log(lo), math.log(hi)))))
+    groups, m = log(1, 40), log(1, 6000)
+    rows, cols = ([log(1, 900), r.choice([8, 16, 24, 64, 72, 128])] if r.random() < 0.5 else [log(1, 700), log(1, 1100)])
+    if r.random() < 0.5:
+        rows, cols = cols, rows
+    gen = gen_of(1000 + seed)
+    which = torch.sort(torch.randint(groups, (m,), generator=gen, device="cuda"))[0]
+    off = torch.searchsorted(which, torch.arange(groups + 1, device="cuda")).to(torch.int32)
+    at, st = off.tolist(), new_status()
+    ldw, ldx, ldy = up8(cols), up8(cols), up8(rows)
+    W, X, dY = padded(gen, groups * rows, cols, ldw, std=0.1), padded(gen, m, cols, ldx), padded(gen, m, rows, ldy)
+    for fp32 in (0, 1):
+        t = torch.float32 if fp32 else torch.bfloat16
+        Y, dX, dW = sentinel(m, ldy, t), sentinel(m, ldx, t), sentinel(groups * rows, ldw, t)
+        B.mwu_gemm_grouped(groups, rows, cols, W, ldw, rows * ldw, off, X, m, ldx, Y, ldy, fp32, st)
+        B.mwu_gemm_grouped_dx(groups, rows, cols, W, ldw, rows * ldw, off, dY, m, ldy, dX, ldx, fp32, st)
+        B.mwu_gemm_grouped_dw(groups, rows, cols, off, dY, m, ldy, X, ldx, dW, ldw, rows * ldw, fp32, 0, st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        assert bool((Y[:, rows:] == 777).all() & (dX[:, cols:] == 777).all() & (dW[:, cols:] == 777).all())
+        for g in range(groups):
+            rng, mine = slice(at[g], at[g + 1]), slice(g * rows, (g + 1) * rows)
+            x, d, w = X[rng, :cols].to(F64), dY[rng, :rows].to(F64), W[mine, :cols].to(F64)
+            check(Y[rng, :rows], x @ w.t(), x.abs() @ w.t().abs(), cols, fp32)
+            check(dX[rng, :cols], d @ w, d.abs() @ w.abs(), rows, fp32)
+            check(dW[mine, :cols], d.t() @ x, d.t().abs() @ x.abs(), max(1, at[g + 1] - at[g]), fp32)
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
