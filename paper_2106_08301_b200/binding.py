@@ -142,17 +142,22 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return torch.cuda.current_stream().cuda_stream
 
 
-def _operands(device: int, *tensors):
-    """Addresses of (tensor or None, type) pairs, each of that type, contiguous and on `device`: a kernel reads what it is given as its own type."""
-    out = []
-    for t, dtype in tensors:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype != dtype or not t.is_contiguous() or t.get_device() != device:
-            raise ValueError(f"contiguous {dtype} tensors of the current device only: got {t.dtype} on {t.device}")
-        out.append(t.data_ptr())
-    return out
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _address(t: Optional[torch.Tensor], dtype, device: int):
+    """The address of a contiguous tensor of this type on this device, or None: a kernel reads what it is given as its own type."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"contiguous {dtype} tensors of the current device only: got {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _stream_on(stream: Optional[torch.cuda.Stream], device: int):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def status_string(status: int) -> str:
@@ -309,9 +314,10 @@ _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 def mwu_gemm_grouped(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, Y, ldy, y_dtype, dev_status, stream=None,
                      check=True) -> int:
     """Y[m] = X[m] W_g^T for the rows m of every group g."""
-    w, o, x, y, st = _operands(torch.cuda.current_device(), (Wd, _BF16), (offsets, _I32), (X, _BF16), (Y, _F32 if y_dtype else _BF16),
-                               (dev_status, _I32))
-    rc = lib().mwu_gemm_grouped(groups, rows, cols, w, ldw, w_stride, o, x, M, ldx, y, ldy, y_dtype, st, _stream(stream))
+    d = _get_device()
+    rc = lib().mwu_gemm_grouped(groups, rows, cols, _address(Wd, _BF16, d), ldw, w_stride, _address(offsets, _I32, d),
+                                _address(X, _BF16, d), M, ldx, _address(Y, _F32 if y_dtype else _BF16, d), ldy, y_dtype,
+                                _address(dev_status, _I32, d), _stream_on(stream, d))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped")
     return rc
@@ -320,9 +326,10 @@ def mwu_gemm_grouped(groups, rows, cols, Wd, ldw, w_stride, offsets, X, M, ldx, 
 def mwu_gemm_grouped_dx(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, lddy, dX, lddx, dx_dtype, dev_status,
                         stream=None, check=True) -> int:
     """dX[m] = dY[m] W_g for the rows m of every group g."""
-    w, o, d, x, st = _operands(torch.cuda.current_device(), (Wd, _BF16), (offsets, _I32), (dY, _BF16), (dX, _F32 if dx_dtype else _BF16),
-                               (dev_status, _I32))
-    rc = lib().mwu_gemm_grouped_dx(groups, rows, cols, w, ldw, w_stride, o, d, M, lddy, x, lddx, dx_dtype, st, _stream(stream))
+    d = _get_device()
+    rc = lib().mwu_gemm_grouped_dx(groups, rows, cols, _address(Wd, _BF16, d), ldw, w_stride, _address(offsets, _I32, d),
+                                   _address(dY, _BF16, d), M, lddy, _address(dX, _F32 if dx_dtype else _BF16, d), lddx, dx_dtype,
+                                   _address(dev_status, _I32, d), _stream_on(stream, d))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped_dx")
     return rc
@@ -331,10 +338,10 @@ def mwu_gemm_grouped_dx(groups, rows, cols, Wd, ldw, w_stride, offsets, dY, M, l
 def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, lddw, dw_stride, dw_dtype, accumulate,
                         dev_status, stream=None, check=True) -> int:
     """dW_g = dY_g^T X_g (accumulate: added to dW_g)."""
-    o, d, x, w, st = _operands(torch.cuda.current_device(), (offsets, _I32), (dY, _BF16), (X, _BF16), (dW, _F32 if dw_dtype else _BF16),
-                               (dev_status, _I32))
-    rc = lib().mwu_gemm_grouped_dw(groups, rows, cols, o, d, M, lddy, x, ldx, w, lddw, dw_stride, dw_dtype, accumulate, st,
-                                   _stream(stream))
+    d = _get_device()
+    rc = lib().mwu_gemm_grouped_dw(groups, rows, cols, _address(offsets, _I32, d), _address(dY, _BF16, d), M, lddy,
+                                   _address(X, _BF16, d), ldx, _address(dW, _F32 if dw_dtype else _BF16, d), lddw, dw_stride,
+                                   dw_dtype, accumulate, _address(dev_status, _I32, d), _stream_on(stream, d))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_gemm_grouped_dw")
     return rc
@@ -343,11 +350,11 @@ def mwu_gemm_grouped_dw(groups, rows, cols, offsets, dY, M, lddy, X, ldx, dW, ld
 def mwu_adapters_add(adapters, rank, rows, cols, A, lda, a_stride, Bm, ldb, b_stride, scale, segments, offsets, which, X, M,
                      ldx, Y0, Y, ldy, y_dtype, dev_status, stream=None, check=True) -> int:
     """Y = Y0 + scale (X A^T) B^T for segments of rows with an adapter each (Y0 None: zeros; Y itself: in place)."""
-    out = _F32 if y_dtype else _BF16
-    a, b, sc, o, w, x, y0, y, st = _operands(torch.cuda.current_device(), (A, _BF16), (Bm, _BF16), (scale, _F32), (offsets, _I32),
-                                             (which, _I32), (X, _BF16), (Y0, out), (Y, out), (dev_status, _I32))
-    rc = lib().mwu_adapters_add(adapters, rank, rows, cols, a, lda, a_stride, b, ldb, b_stride, sc, segments, o, w, x, M, ldx, y0, y,
-                                ldy, y_dtype, st, _stream(stream))
+    d, out = _get_device(), _F32 if y_dtype else _BF16
+    rc = lib().mwu_adapters_add(adapters, rank, rows, cols, _address(A, _BF16, d), lda, a_stride, _address(Bm, _BF16, d), ldb,
+                                b_stride, _address(scale, _F32, d), segments, _address(offsets, _I32, d), _address(which, _I32, d),
+                                _address(X, _BF16, d), M, ldx, _address(Y0, out, d), _address(Y, out, d), ldy, y_dtype,
+                                _address(dev_status, _I32, d), _stream_on(stream, d))
     if check and rc != MWU_OK:
         raise MwuError(rc, "mwu_adapters_add")
     return rc

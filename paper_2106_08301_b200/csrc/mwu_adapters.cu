@@ -14,6 +14,12 @@
 //                             the tensor work is nothing; a lane's eight consecutive elements stand for a permuted reduction order)
 //   mwu_adapters_tile_kernel  128 rows to a cluster of 1 to 8 CTAs, TMA and tcgen05.mma, Y0 and Y through shared memory
 //
+// What bounds them (us a call among others).  Few rows: latency.  One row, rank 16, 4096 -> 4096: 5 on the device (list 1.1, first product 0.7, adding
+// it up 1.7, second 0.8), 8.5 with the host.  64 rows of 32 adapters, rank 32, 4096 -> 16384: 16.9 (3 to sort, 2.5, 3, 5); 73 before loads stood ahead of
+// tests of their values, 35 before rows were sorted by adapter, 19 with one run of columns at a time; B and Y0 brought to L2 ahead: no
+// faster, and 1 us to ask for.  Many rows: HBM.  8192 rows, rank 64, 4096 -> 4096: 48.5 (X in at 4.1 TB/s, 5 us to add up T, Y0 in and Y out at 5.4).
+// Rows without an adapter are copied with eight loads in flight (one: 72 instead of 45 us for that tile).
+//
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises MWU_DEV_TIMEOUT, waits for its copies in
 // flight, frees tensor memory and returns.
 #include "mwu_rows.cuh"

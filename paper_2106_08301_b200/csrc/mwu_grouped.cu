@@ -15,15 +15,24 @@
 // and a lane of tensor memory is a feature, so a warp's store of one line is one contiguous run of the output, whatever
 // the line: ragged groups need no masked box, only a test per line.
 // The groups' offsets are checked and turned into a table of tiles by every CTA at its start (device memory, no host).
-// In the weight gradient a group's last stage of 64 rows may hold rows of the next group, which must not be multiplied, not
-// even by zero (they may be NaN): such a stage is loaded onto a barrier of its own, a warp of each CTA zeroes the
+// In the weight gradient a group's last block of 64 rows may hold rows of the next group, which must not be multiplied, not
+// even by zero (they may be NaN): its stage is loaded onto a barrier of its own, a warp of each CTA zeroes the
 // foreign rows up to the next multiple of 16 in both operands, and only then it is handed to the issuer of the MMAs.
 // fp32 results: the tensor core drops what lies below an accumulator's last place (about 1e-9 of the result a product, always
 // towards zero), so sums are taken out of tensor memory every 512 products and added in registers; bf16 results hide it.
 //
+// What bounds it (us a pass among others).  Many rows: the power cap and the loads of full tiles.  16 of 4096 x 4096, 16384 rows: 461,
+// 1.19 PFLOP/s (300 to 357 without the loads); input gradient of 8192 rows 266, alone and cool 217 with the tensor pipe at 70 % and the
+// crossbar at 41 %.  Weight gradients: the fp32 output besides (16 of 2048 x 4096: 325, 253 without the stores; a burst of them
+// from all SMs leaves at 5.8 TB/s).  Few rows: reading the weights (64 of 2048 x 4096, 256 rows: 166, 5.9 TB/s).  Small calls: 2.5 us until the
+// roles begin, 2.3 until the first stage is there, 2 to 3 from the last MMA to the last store, and 0.27 us a stage whatever is in it.
+// Tried and taken back: weights or activations brought to L2 ahead of their loads (4 to 17 % slower: the copy engine's requests are what
+// is short); tiles of a pair worked out in a table before the first load, and the epilogue's code in one loop (a small call 1.3 us
+// slower); six stages with one output box a warp, and three boxes (no change).
+//
 // Roles per CTA (11 warps): warp 0 TMA producer, warp 1 tensor memory and (leader) MMAs, warps 2 to 9 epilogue (two per
 // 32-lane quarter, every other 32 lines), warp 10 zeroes foreign rows.  Every wait on an mbarrier is bounded; when one runs
-// out the kernel raises MWU_DEV_TIMEOUT, drains what it issued, frees tensor memory and returns.
+// out the kernel raises MWU_DEV_TIMEOUT, lets its loads land, frees tensor memory and returns.
 #include "mwu_rows.cuh"
 
 namespace mwu {
@@ -40,7 +49,7 @@ constexpr int G_SIDE = 128 * 128;                    // bytes of 128 features or
 constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 64 reduction steps
 constexpr int G_BOX = 2048;                          // of output: 32 features x 16 lines of fp32, x 32 of bf16; two to a warp
 constexpr int G_BAND = 8;                            // line tiles per band of the tile order
-constexpr int G_CHUNK = 8;                           // stages between two sums of an fp32 result (512 products)
+constexpr int G_CHUNK = 8;                           // blocks of 64 between two sums of an fp32 result (512 products)
 
 enum { G_FORWARD = 0, G_DX = 1, G_DW = 2 };
 
@@ -461,8 +470,8 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
             }
             if (!ok) break;
             const int f0 = t.feature0 + (int)rank * 128 + quarter * 32, f = f0 + lane;
-            // Output through boxes in shared memory where it is whole boxes (the map clips a store at 16 bytes, and at the last
-            // weight row, but not at the end of a group of lines).
+            // Output through boxes in shared memory and TMA, 40 GB/s an SM (plain stores 14 a word a lane, 21 at 16 bytes), where it is whole
+            // boxes: the map clips a store at 16 bytes, and at the last weight row, but not at the end of a group of lines.
             const bool boxed = f0 + 32 <= p.features || p.features % (p.out_fp32 ? 4 : 8) == 0;
             // (accumulating: a group without rows adds nothing)
             const int lines = f0 >= p.features || (OP == G_DW && p.accumulate && n_st == 0) ? 0 : t.line_count;
@@ -635,8 +644,11 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     CUtensorMap tmap_f;
     LineMaps maps_l;
     if (!encode_bf16(encode, &tmap_f, Wd, cols, rows, ldw, OP == G_FORWARD ? p.feature_box : 64, groups, w_stride)) return MWU_ERR_CUDA;
-    for (int b = 0; b < 3; ++b)
+    for (int b = 2; b >= 0; --b) {
+        maps_l.m[b] = maps_l.m[2];                          // (a larger box than any tile takes: never used)
+        if (b < 2 && p.line_tile <= (b ? 64 : 192)) continue;
         if (!encode_bf16(encode, &maps_l.m[b], in, red, M, ldi, 128 >> b, 0, 0)) return MWU_ERR_CUDA;
+    }
     CUtensorMap tmap_out;
     if (!encode_out(encode, &tmap_out, out, out_dtype != 0, features, M, ldo, 0, 0)) return MWU_ERR_CUDA;
     return launch_grouped<OP>(tmap_f, maps_l, tmap_out, p, most, sm_count, (cudaStream_t)cuda_stream) == cudaSuccess ? MWU_OK : MWU_ERR_CUDA;

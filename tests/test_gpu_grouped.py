@@ -243,6 +243,20 @@ def test_offsets_that_make_no_sense_write_nothing(at):
     assert bool((Y == 777).all() & (dX == 777).all() & (dW == 777).all())
 
 
+def test_the_binding_refuses_other_types_and_places():
+    gen, st = gen_of(1), new_status()
+    W, X, Y, off = normal(gen, 2, 24, 40), normal(gen, 9, 40), torch.zeros(9, 24, device="cuda"), torch.tensor([0, 4, 9], dtype=torch.int32, device="cuda")
+    good = dict(groups=2, rows=24, cols=40, Wd=W, ldw=40, w_stride=960, offsets=off, X=X, M=9, ldx=40, Y=Y, ldy=24, y_dtype=1, dev_status=st)
+    for change in (dict(offsets=off.long()), dict(Wd=W.float()), dict(X=X.half()), dict(y_dtype=0), dict(Y=Y.t()), dict(X=X.cpu()), dict(dev_status=st.float())):
+        with pytest.raises(ValueError):
+            B.mwu_gemm_grouped(**{**good, **change})
+    with pytest.raises(B.MwuError):
+        B.mwu_gemm_grouped(**{**good, "ldw": 36})
+    B.mwu_gemm_grouped(**good)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+
+
 def test_no_rows():
     gen, rows, cols = gen_of(2), 24, 40
     off, st = torch.zeros(3, dtype=torch.int32, device="cuda"), new_status()
