@@ -375,7 +375,8 @@ int mwu_gemm_dense(int64_t rows, int64_t cols, const void *Wd, int64_t ldw, cons
  * Leading dimensions and group strides are multiples of 8 elements (fp32 outputs: of 4).  M == 0 is a no-op for the first two; the
  * third then still writes its zeros.  Outputs must not overlap inputs.
  * Products are bf16 x bf16 accumulated in fp32; fp32 results are summed in pieces of 512 products, so that what the
- * tensor core drops of a long sum stays below 1e-6 of it.  The same call on the same inputs gives the same bits.
+ * tensor core drops of a long sum stays below 1e-6 of it, bf16 results in pieces of 262144.  The same call on the same inputs
+ * gives the same bits.
  */
 #define MWU_MAX_GROUPS 1024
 #define MWU_MAX_GROUPED_SIDE 1048576
@@ -408,7 +409,7 @@ int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, const int32_
  *   Y0           in   its output, [M][ldy >= rows], of Y's type; may be Y itself (added in place) or NULL (zeros), and must not
  *                     overlap Y otherwise
  *   Y            out  [M][ldy]; y_dtype 0: bf16, 1: fp32.  Rows of no segment are left as they are.
- * 1 <= rank <= MWU_MAX_RANK, segments <= MWU_MAX_SEGMENTS, rows and cols <= MWU_MAX_GROUPED_SIDE, of any value; lda, ldb, ldx, a_stride,
+ * M == 0 or segments == 0 is a no-op.  1 <= rank <= MWU_MAX_RANK, segments <= MWU_MAX_SEGMENTS, rows and cols <= MWU_MAX_GROUPED_SIDE, of any value; lda, ldb, ldx, a_stride,
  * b_stride and a bf16 ldy are multiples of 8 elements, an fp32 ldy of 4.  X A^T is held in fp32 and enters the second product as
  * bf16 terms (two for a bf16 Y, three for fp32), so no rounding but Y's own shows.  The same call on the same
  * inputs gives the same bits.  For training, the gradients are grouped products with a side as long as the rank, of the rows sorted

@@ -50,6 +50,7 @@ constexpr int G_SUB = 64 * 128;                      // MN-major: 64 features x 
 constexpr int G_BOX = 2048;                          // of output: 32 features x 16 lines of fp32, x 32 of bf16; two to a warp
 constexpr int G_BAND = 8;                            // line tiles per band of the tile order
 constexpr int G_CHUNK = 8;                           // blocks of 64 between two sums of an fp32 result (512 products)
+constexpr int G_CHUNK_BF16 = 4096;                   // ... of a bf16 result: 262144 products lose 3e-4 of it and take 1 ms
 
 enum { G_FORWARD = 0, G_DX = 1, G_DW = 2 };
 
@@ -90,6 +91,7 @@ __device__ __forceinline__ void tma_load_3d_pair(unsigned dst, const CUtensorMap
         "[%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(bar_cluster), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, unsigned src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
@@ -212,7 +214,12 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         sm->abort = 0;
         sm->drain_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&tmap_f);
+        prefetch_map(&tmap_out);
+        for (int b = 0; b < (OP == G_DW ? 1 : 3); ++b) prefetch_map(&maps_l.m[b]);
     }
+    __syncwarp();
+    cluster_arrive();                                   // both CTAs' barriers exist before any remote arrive: waited for below
     if (warp == 1) tmem_alloc2(smem_u32(&sm->tmem_base), 512);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // the groups: offsets in order and inside the rows that there are, or nothing is done at all
@@ -252,7 +259,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                                 // both CTAs' barriers exist before any remote arrive
+    cluster_wait();
     tc_fence_after();
     const unsigned tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile unsigned *>(&sm->tmem_base), 0);
     // (the host refuses sizes whose tile count could pass 2^31)
@@ -336,7 +343,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         bool ok = true;
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
-            const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_blk = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_blk;
+            const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_blk = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : G_CHUNK_BF16;
             const unsigned idesc = make_idesc_pair(__shfl_sync(0xffffffffu, t.line_pad, 0)) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
             for (int c0 = 0; ok && c0 < n_blk; c0 += chunk, ++use) {
                 const unsigned buf = use & 1u;
@@ -441,7 +448,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         };
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
-            const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : n_st;
+            const int n_st = (t.red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : G_CHUNK_BF16;
             float acc[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q)

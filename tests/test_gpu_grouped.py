@@ -336,6 +336,23 @@ def test_fp32_sums_of_long_reductions():
     assert float((Y.to(F64) - ref).norm() / ref.norm()) < 1e-6
 
 
+def test_bf16_sums_of_very_long_reductions():
+    """More rows than go into one piece of a bf16 sum (262144), by whole numbers whose sums a bf16 result holds exactly."""
+    m, rows, cols = 600011, 8, 16
+    gen = gen_of(12)
+    which = torch.randint(0, m, (40,), generator=gen, device="cuda")
+    d, x = torch.zeros(m, rows, dtype=torch.bfloat16, device="cuda"), torch.zeros(m, cols, dtype=torch.bfloat16, device="cuda")
+    d[which] = torch.randint(-2, 3, (40, rows), generator=gen, device="cuda").to(torch.bfloat16)
+    x[which] = torch.randint(-1, 2, (40, cols), generator=gen, device="cuda").to(torch.bfloat16)
+    off, st = torch.tensor([0, 11, 600000], dtype=torch.int32, device="cuda"), new_status()
+    dW = torch.zeros(2, rows, cols, dtype=torch.bfloat16, device="cuda")
+    B.mwu_gemm_grouped_dw(2, rows, cols, off, d, m, rows, x, cols, dW, cols, rows * cols, 0, 0, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    for g, r in enumerate((slice(0, 11), slice(11, 600000))):
+        assert torch.equal(dW[g].to(F64), d[r].to(F64).t() @ x[r].to(F64))      # below 256 in magnitude: 40 products of at most 2
+
+
 def test_positions_beyond_32_bits():
     gen, rows, cols = gen_of(4), 64, 64
     m, ld = 70000, 32768                                    # the last rows start past 2^31 elements
