@@ -8,7 +8,7 @@
 // distributed shared memory, and share the columns of the second (a slice of rows of B each); T is held in fp32 and enters the
 // second product as two bf16 terms, three where Y is fp32 (2^-18, 2^-27 of it), so that only Y's own rounding shows.
 //
-// Segments of up to FEW_ROWS rows (generation) and longer ones (prompts) take different kernels, both decide on the
+// Segments of up to FEW_ROWS rows (generation) and longer ones (prompts) take different kernels (up to FEW_IN_ALL rows in all, the first), both decide on the
 // device which segments are theirs, and where both are launched they run at the same time:
 //   mwu_adapters_few_kernel   16 rows to a cluster of 8 CTAs, mma.sync straight from global memory (the operands are read once and
 //                             the tensor work is nothing; a lane's eight consecutive elements stand for a permuted reduction order)
@@ -33,9 +33,9 @@ namespace adapters {
 using namespace gemm;
 
 constexpr int FEW_ROWS = 32;            // rows of a segment that the first kernel takes,
-constexpr int FEW_IN_ALL = 256;         // and rows of a call that it takes whatever its segments, sorted by adapter
+constexpr int FEW_IN_ALL = 256;         // rows of a call that it takes whatever its segments,
+constexpr int SORTED_ROWS = 512;        // and rows of a call that it sorts by adapter
 constexpr int FEW_THREADS = 256;
-static_assert(FEW_IN_ALL == FEW_THREADS, "a thread sorts one row");
 constexpr int TILE_THREADS = 320;
 constexpr int TILE_ROWS = 128;          // rows of an item of the tile kernel
 
@@ -48,6 +48,7 @@ struct Params {
     void *Y;
     int adapters, rank, rows, cols, segments, M;
     int few_rows;                       // FEW_ROWS, or as many as may be
+    int sorted;                         // the few-rows kernel's rows are sorted by adapter
     int beside;                         // the few-rows kernel runs beside the tile kernel launched before it
     unsigned *dev_status;
 };
@@ -115,56 +116,69 @@ __device__ __forceinline__ void find_item(const Params &p, Finder *f, int per, i
     }
 }
 
-// A call of few rows in all is worked on adapter by adapter, 16 rows at a time, wherever in the batch they are: 64 tokens of 32
-// adapters read every adapter once, not twice.
+// Up to SORTED_ROWS rows of a call are worked on adapter by adapter, 16 rows at a time, wherever in the batch they are: 64 tokens of 32
+// adapters read every adapter once, not twice (4096 -> 16384: 17 us instead of 35), and 512 tokens of 4 adapters once for 16 rows.
 struct Sorter {
-    int key[FEW_THREADS];               // adapter of a row; NOBODY: of no segment
-    int row[FEW_THREADS];               // rows in the order of their adapters
-    int start[FEW_THREADS + 1];         // where an item's rows start in `row`
-    unsigned starts[FEW_THREADS / 32];
+    int key[SORTED_ROWS];               // adapter of a row; NOBODY: not this kernel's
+    int row[SORTED_ROWS];               // rows in the order of their adapters
+    int start[SORTED_ROWS + 1];         // where an item's rows start in `row`
+    unsigned starts[SORTED_ROWS / 32];
     int counted;
 };
 constexpr int NOBODY = 0x7fffffff;
 
-// returns the number of items, -1 where the list makes no sense.  All threads of the CTA.
+// Returns the number of items, -1 where the list makes no sense.  All threads of the CTA, each placing two rows by counting those that
+// come before them.  (A bitonic sort is a barrier a step: 3.4 us more for 64 rows.  Single tokens, 4 adapters, rank 32, 4096 -> 16384, sorted /
+// segment by segment: 257 rows 25 us / 64, 384 34 / 94, 512 52 / 114.)
 __device__ __forceinline__ int sort_rows(const Params &p, Sorter *o, int per) {
+    constexpr int MINE = SORTED_ROWS / FEW_THREADS;
     const int tid = threadIdx.x;
-    o->key[tid] = NOBODY;
-    if (tid < FEW_THREADS / 32) o->starts[tid] = 0u;
+#pragma unroll
+    for (int q = 0; q < MINE; ++q) o->key[tid + q * FEW_THREADS] = NOBODY;
+    if (tid < SORTED_ROWS / 32) o->starts[tid] = 0u;
     if (tid == 0) o->counted = 0;
     __syncthreads();
-    int bad = 0;
+    int bad = 0, rows = 0;
     for (int s = tid * per; s < (tid + 1) * per && s < p.segments; ++s) {
         const int a = __ldg(p.offsets + s), b = __ldg(p.offsets + s + 1), w = __ldg(p.which + s);
         const bool wrong = a < 0 || b < a || b > p.M || w < -1 || w >= p.adapters;
         bad |= wrong;
-        if (!wrong)
+        if (!wrong && b - a <= p.few_rows) {
+            rows += b - a;
             for (int r = a; r < b; ++r) o->key[r] = w;
+        }
     }
+    if (rows) atomicAdd(&o->counted, rows);
     if (__syncthreads_or(bad)) return -1;
-    const int mine = o->key[tid];
-    int less = 0, same = 0;                                 // rows of smaller adapters; of mine, before this one
-    for (int j = 0; j < p.M; j += 4) {
-        const int4 k = *reinterpret_cast<const int4 *>(&o->key[j]);
-        less += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
-        same += (k.x == mine && j < tid) + (k.y == mine && j + 1 < tid) + (k.z == mine && j + 2 < tid) + (k.w == mine && j + 3 < tid);
-    }
-    const int at = less + same;
-    const bool counts = mine != NOBODY, first = counts && same % 16 == 0;
-    if (counts) {
-        o->row[at] = tid;
-        atomicAdd(&o->counted, 1);
-    }
-    if (first) atomicOr(&o->starts[at / 32], 1u << (at % 32));
-    __syncthreads();
-    int before = 0, total = 0;
+    if (o->counted == 0) return 0;                          // all of them the other kernel's
+    int at[MINE];
+    bool first[MINE];
 #pragma unroll
-    for (int w = 0; w < FEW_THREADS / 32; ++w) {
-        const unsigned v = o->starts[w];
-        before += __popc(w < at / 32 ? v : (w == at / 32 ? v & ((1u << (at % 32)) - 1u) : 0u));
-        total += __popc(v);
+    for (int q = 0; q < MINE; ++q) {
+        const int r = tid + q * FEW_THREADS, mine = o->key[r];
+        int less = 0, same = 0;                             // rows of smaller adapters; of mine, before this one
+        if (mine != NOBODY)
+            for (int j = 0; j < p.M; j += 4) {
+                const int4 k = *reinterpret_cast<const int4 *>(&o->key[j]);
+                less += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+                same += (k.x == mine && j < r) + (k.y == mine && j + 1 < r) + (k.z == mine && j + 2 < r) + (k.w == mine && j + 3 < r);
+            }
+        at[q] = less + same;
+        first[q] = mine != NOBODY && same % 16 == 0;
+        if (mine != NOBODY) o->row[at[q]] = r;
+        if (first[q]) atomicOr(&o->starts[at[q] / 32], 1u << (at[q] % 32));
     }
-    if (first) o->start[before] = at;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < SORTED_ROWS / 32; ++w) total += __popc(o->starts[w]);
+#pragma unroll
+    for (int q = 0; q < MINE; ++q)
+        if (first[q]) {
+            int before = __popc(o->starts[at[q] / 32] & ((1u << (at[q] % 32)) - 1u));
+            for (int w = 0; w < at[q] / 32; ++w) before += __popc(o->starts[w]);
+            o->start[before] = at[q];
+        }
     if (tid == 0) o->start[total] = o->counted;
     __syncthreads();
     return total;
@@ -273,9 +287,8 @@ mwu_adapters_few_kernel(const Params p) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int c = (int)cluster_rank(), ctas = (int)cluster_size(), clusters = (int)gridDim.x / ctas;
     const int per = (p.segments + FEW_THREADS - 1) / FEW_THREADS;
-    const bool sorted = p.few_rows != FEW_ROWS;
     int first = 0;
-    const int total = sorted ? sort_rows(p, &find.o, per) : count_items<true, FEW_THREADS>(p, &f, per, first);
+    const int total = p.sorted ? sort_rows(p, &find.o, per) : count_items<true, FEW_THREADS>(p, &f, per, first);
     if (total < 0 && blockIdx.x == 0 && tid == 0) atomicOr(p.dev_status, (unsigned)MWU_DEV_BOUNDS);
     const int k_chunks = (p.cols + 31) / 32, n_groups = (p.rows + 31) / 32;
     const int kc0 = (int)((long long)k_chunks * c / ctas), kc1 = (int)((long long)k_chunks * (c + 1) / ctas);
@@ -284,7 +297,7 @@ mwu_adapters_few_kernel(const Params p) {
     for (int item = (int)blockIdx.x / ctas; item < total; item += clusters) {
         int row0 = 0, count, a;
         const int *rows = nullptr;
-        if (sorted) {
+        if (p.sorted) {
             const int at = find.o.start[item];
             count = find.o.start[item + 1] - at;
             rows = &find.o.row[at];
@@ -1005,12 +1018,14 @@ static cudaError_t launch_few(const Params &p, int sm_count, cudaStream_t st) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     // a cluster for every 16 rows that there may be of a segment or an adapter, as far as four CTAs an SM go; more items are taken in turn
-    long long items = p.M / 16 + (p.few_rows == FEW_ROWS ? (long long)p.segments : p.adapters + 1ll);
-    if (p.few_rows == FEW_ROWS && items > 2ll * p.segments) items = 2ll * p.segments;
+    long long items = p.M / 16 + (p.sorted ? p.adapters + 1ll : (long long)p.segments);
+    if (!p.sorted && items > 2ll * p.segments) items = 2ll * p.segments;
     if (items > p.M) items = p.M;
-    // CTAs to a cluster: as many as leave the SMs with two or three (64 rows of 32 adapters, 4096 -> 16384, rank 32: 16.6 us with eight,
-    // 19.9 with six, 20.4 with four; beside 2777 rows of prompts, 61 rows, 1216 -> 1000: 23.6 with two, 24.4 / 31.1 with four / eight)
-    long long ctas = 5ll * sm_count / (2 * items);
+    // CTAs to a cluster: as many as leave the SMs with two (of those that are to be expected: half of the adapters in use).  64 rows of 32
+    // adapters, 4096 -> 16384, rank 32: 16.6 us with eight, 19.9 with six, 20.4 with four; beside 2777 rows of prompts, 61 rows, 1216 ->
+    // 1000: 23.6 with two, 24.4 / 31.1 with four / eight.
+    const long long expected = p.sorted ? p.M / 16 + ((p.adapters + 1ll < p.M ? p.adapters + 1ll : p.M) + 1) / 2 : items;
+    long long ctas = 7ll * sm_count / (4 * expected);
     ctas = ctas < 2 ? 2 : ctas > 8 ? 8 : ctas;
     const long long most = 4ll * sm_count / ctas;
     count_launch();
@@ -1097,6 +1112,7 @@ static int launch_tile(const Params &p, int sm_count, cudaStream_t st) {
 template <int R, bool F32>
 static int launch_both(Params p, int sm_count, cudaStream_t st) {
     p.few_rows = 0x7fffffff;
+    p.sorted = p.M <= SORTED_ROWS;
     if (p.M > FEW_IN_ALL) {
         p.few_rows = FEW_ROWS;
         const int rc = launch_tile<R, F32>(p, sm_count, st);

@@ -155,6 +155,37 @@ def test_rows_of_one_adapter_all_over_the_batch():
         b.check(Z, b.Y0, b.Y0)
 
 
+@pytest.mark.parametrize("lengths", [[1] * 257, [1] * 512, [1] * 513, [1] * 100 + [200] + [5] * 20 + [1] * 100, [1] * 1025, [32] * 16, [33] * 15 + [1],
+                                     [31, 0, 33, 1] * 7 + [2] * 20], ids=lambda x: f"{len(x)}of{sum(x)}")
+@pytest.mark.parametrize("adapters,fp32", [(1, 0), (7, 1), (40, 0)])
+def test_batches_of_several_hundred_rows(lengths, adapters, fp32):
+    """Rows of short segments are sorted by adapter up to 512 rows, beside the prompts; above, segment by segment."""
+    r = random.Random(len(lengths) + adapters)
+    b = Batch(lengths, [r.randrange(-1, adapters) for _ in lengths], adapters, 24, 72, 200, fp32, first=1 if sum(lengths) < 1024 else 0)
+    Z = b.Y0.clone()
+    b.run(Z, Z)
+    torch.cuda.synchronize()
+    assert int(b.st.item()) == 0
+    # the formula for all rows at once, as in Batch.check
+    seg = torch.repeat_interleave(torch.arange(len(lengths)), torch.tensor(lengths))
+    a = torch.tensor(b.which_list)[seg].cuda()
+    on, a = (a >= 0), a.clamp(min=0)
+    rows = slice(b.at[0], b.at[-1])
+    x, w, bm = b.X[rows, :200].to(F64), b.A[:, :24, :200].to(F64)[a], b.B[:, :72, :24].to(F64)[a]
+    sc = b.scale.to(F64)[a] * on
+    t = torch.einsum("mk,mrk->mr", x, w)
+    base = b.Y0[rows, :72].to(F64)
+    ref = base + sc[:, None] * torch.einsum("mr,mnr->mn", t, bm)
+    S = sc.abs()[:, None] * torch.einsum("mr,mnr->mn", t.abs(), bm.abs())
+    S2 = sc.abs()[:, None] * torch.einsum("mr,mnr->mn", torch.einsum("mk,mrk->mr", x.abs(), w.abs()), bm.abs())
+    terms = 3 if fp32 else 2
+    tol = (64 * 2.0 ** -23 + (200 / 512 + 10) * 2.0 ** -24) * S2 + S * (2.0 ** (-17 if terms == 2 else -25) + 2.5 * terms * 2.0 ** -22)
+    tol = tol + (ref.abs() + base.abs()) * 2.0 ** -23 + (0 if fp32 else ref.abs() * 2.0 ** -8)
+    got = Z[rows, :72]
+    assert bool(((got.to(F64) - ref).abs() <= tol + 1e-30).all())
+    assert torch.equal(got[~on], b.Y0[rows, :72][~on]) and torch.equal(Z[:, 72:], b.Y0[:, 72:]) and torch.equal(Z[:b.at[0]], b.Y0[:b.at[0]])
+
+
 def test_without_scales_and_without_padding():
     for lengths in ([1, 1, 4], [200, 1]):
         b = Batch(lengths, [0] * len(lengths), 1, 16, 128, 256, 0, pad=False, with_scale=False)
