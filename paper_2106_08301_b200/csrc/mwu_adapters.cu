@@ -246,6 +246,20 @@ __device__ __forceinline__ void keep8(uint4 &v, int valid) {
     v.z = keep_valid(v.z, 4, valid);
     v.w = keep_valid(v.w, 6, valid);
 }
+// The next bf16 term of s, and s without it.  An infinity leaves nothing (inf - inf would make NaN of it), and what would round to an
+// infinity without being one goes to the largest bf16 (its remainder is below 2^120).
+__device__ __forceinline__ float next_term(float &s) {
+    float h = __bfloat162float(__float2bfloat16_rn(s));
+    if (isinf(h)) {
+        if (isinf(s)) {
+            s = 0.f;
+            return h;
+        }
+        h = copysignf(0x1.fep127f, h);
+    }
+    s -= h;
+    return h;
+}
 __device__ __forceinline__ float remote_f32(unsigned local, unsigned cta) {
     unsigned at;
     float v;
@@ -434,12 +448,9 @@ mwu_adapters_few_kernel(const Params p) {
 #pragma unroll 4
             for (int o = 0; o < ctas; ++o) s += remote_f32(smem_u32(&(&sm->part[0][0])[e]), (unsigned)o);
             s *= scale;
+            if (e % R >= p.rank) s = 0.f;                   // (an infinity of X times the zeros that stand for A there is NaN)
 #pragma unroll
-            for (int q = 0; q < TERMS; ++q) {
-                const __nv_bfloat16 h = __float2bfloat16_rn(s);
-                sm->T[q][e / R][e % R] = h;
-                s -= __bfloat162float(h);
-            }
+            for (int q = 0; q < TERMS; ++q) sm->T[q][e / R][e % R] = __float2bfloat16_rn(next_term(s));
         }
         cluster_arrive();                                   // the others' sums have been read; waited for below
         __syncthreads();
@@ -838,16 +849,15 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             auto give = [&](float (&f)[8], int r, int q8, int o0, int o1) {
                 const unsigned place = smem_u32(sT) + (unsigned)(q8 / 8) * C::ROWS_BYTES + swz((unsigned)r, (unsigned)q8 & 7u);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] *= scale;
+                for (int j = 0; j < 8; ++j) f[j] = 8 * q8 + j < p.rank ? f[j] * scale : 0.f;   // (as in the kernel for few rows)
 #pragma unroll
                 for (int q = 0; q < C::TERMS; ++q) {
                     unsigned w[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+                        const float lo = next_term(f[2 * j]), hi = next_term(f[2 * j + 1]);
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
                         w[j] = *reinterpret_cast<const unsigned *>(&h);
-                        f[2 * j] -= __low2float(h);
-                        f[2 * j + 1] -= __high2float(h);
                     }
 #pragma unroll 1
                     for (int o = o0; o < o1; ++o) {
