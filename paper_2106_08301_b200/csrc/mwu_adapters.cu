@@ -332,68 +332,76 @@ mwu_adapters_few_kernel(const Params p) {
         // this lane's two rows (the first one again where there are fewer: read, never written)
         const long long r0 = row_of(g < count ? g : 0), r1 = row_of(g + 8 < count ? g + 8 : 0);
         // ---- T = X . A^T over this CTA's slice of cols ----
-        float acc[R / 8][4];
-#pragma unroll
-        for (int i = 0; i < R / 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+        // Sums leave the tensor core every 512 products of a warp, as in the kernel for many rows: it drops what lies below an
+        // accumulator's last place, always towards zero (6e-5 of a sum of 65536 products in one piece).
+        constexpr int PIECE = 512 / 32 * (FEW_THREADS / 32);    // chunks of the CTA: up to 8192 columns of two CTAs, one piece
         const __nv_bfloat16 *x0 = p.X + r0 * p.ldx + 8 * t, *x1 = p.X + r1 * p.ldx + 8 * t;
         const __nv_bfloat16 *a0 = p.A + (long long)a * p.a_stride + (long long)g * p.lda + 8 * t;
         constexpr int BATCH = R / 8 < 8 ? R / 8 : 8;        // loads of A in flight, of each of
         constexpr int AHEAD = R <= 32 ? 2 : 1;              // so many chunks
-        for (int ch = kc0 + warp; ch < kc1; ch += AHEAD * (FEW_THREADS / 32)) {
-            uint4 u[AHEAD], v[AHEAD], w[AHEAD][BATCH];
+        int piece = kc0;
+        do {
+            float acc[R / 8][4];
 #pragma unroll
-            for (int i0 = 0; i0 < R / 8; i0 += BATCH) {
+            for (int i = 0; i < R / 8; ++i)
 #pragma unroll
-                for (int h = 0; h < AHEAD; ++h) {
-                    const int cc = ch + h * (FEW_THREADS / 32), k = cc * 32, valid = cc < kc1 ? p.cols - k - 8 * t : 0;
-                    if (i0 == 0) {
-                        u[h] = load8_if(x0 + k, g < count && valid > 0);
-                        v[h] = load8_if(x1 + k, g + 8 < count && valid > 0);
-                    }
+                for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+            const int end = min(kc1, piece + PIECE);
+            for (int ch = piece + warp; ch < end; ch += AHEAD * (FEW_THREADS / 32)) {
+                uint4 u[AHEAD], v[AHEAD], w[AHEAD][BATCH];
 #pragma unroll
-                    for (int i = 0; i < BATCH; ++i)
-                        w[h][i] = load8_if(a0 + (long long)(8 * (i0 + i)) * p.lda + k, 8 * (i0 + i) + g < p.rank && valid > 0);
-                }
+                for (int i0 = 0; i0 < R / 8; i0 += BATCH) {
 #pragma unroll
-                for (int h = 0; h < AHEAD; ++h) {
-                    const int k = (ch + h * (FEW_THREADS / 32)) * 32, valid = p.cols - k - 8 * t;
-                    if (p.cols - k < 32) {
-                        keep8(u[h], valid);
-                        keep8(v[h], valid);
-#pragma unroll
-                        for (int i = 0; i < BATCH; ++i) keep8(w[h][i], valid);
-                    }
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-                        mma_16816(acc[i0 + i], u[h].x, v[h].x, u[h].y, v[h].y, w[h][i].x, w[h][i].y);
-                        mma_16816(acc[i0 + i], u[h].z, v[h].z, u[h].w, v[h].w, w[h][i].z, w[h][i].w);
-                    }
-                }
-            }
-        }
-        // the warps' sums, the upper four onto the lower four first: half the memory
-        float2 *mine = reinterpret_cast<float2 *>(&sm->red[warp % (FEW_THREADS / 64)][g][2 * t]);
-#pragma unroll
-        for (int up = 1; up >= 0; --up) {
-            if (warp / (FEW_THREADS / 64) == up) {
-#pragma unroll
-                for (int i = 0; i < R / 8; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float2 *at = mine + h * 4 * R + 4 * i;          // eight rows on, eight ranks on
-                        float2 v = make_float2(acc[i][2 * h], acc[i][2 * h + 1]);
-                        if (up == 0) {
-                            const float2 o = *at;
-                            v.x += o.x;
-                            v.y += o.y;
+                    for (int h = 0; h < AHEAD; ++h) {
+                        const int cc = ch + h * (FEW_THREADS / 32), k = cc * 32, valid = cc < end ? p.cols - k - 8 * t : 0;
+                        if (i0 == 0) {
+                            u[h] = load8_if(x0 + k, g < count && valid > 0);
+                            v[h] = load8_if(x1 + k, g + 8 < count && valid > 0);
                         }
-                        *at = v;
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i)
+                            w[h][i] = load8_if(a0 + (long long)(8 * (i0 + i)) * p.lda + k, 8 * (i0 + i) + g < p.rank && valid > 0);
                     }
+#pragma unroll
+                    for (int h = 0; h < AHEAD; ++h) {
+                        const int k = (ch + h * (FEW_THREADS / 32)) * 32, valid = p.cols - k - 8 * t;
+                        if (p.cols - k < 32) {
+                            keep8(u[h], valid);
+                            keep8(v[h], valid);
+#pragma unroll
+                            for (int i = 0; i < BATCH; ++i) keep8(w[h][i], valid);
+                        }
+#pragma unroll
+                        for (int i = 0; i < BATCH; ++i) {
+                            mma_16816(acc[i0 + i], u[h].x, v[h].x, u[h].y, v[h].y, w[h][i].x, w[h][i].y);
+                            mma_16816(acc[i0 + i], u[h].z, v[h].z, u[h].w, v[h].w, w[h][i].z, w[h][i].w);
+                        }
+                    }
+                }
             }
-            __syncthreads();
-        }
+            // the warps' sums, the upper four onto the lower four first: half the memory; onto those of the pieces before
+            float2 *mine = reinterpret_cast<float2 *>(&sm->red[warp % (FEW_THREADS / 64)][g][2 * t]);
+#pragma unroll
+            for (int up = 1; up >= 0; --up) {
+                if (warp / (FEW_THREADS / 64) == up) {
+#pragma unroll
+                    for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float2 *at = mine + h * 4 * R + 4 * i;          // eight rows on, eight ranks on
+                            float2 v = make_float2(acc[i][2 * h], acc[i][2 * h + 1]);
+                            if (up == 0 || piece > kc0) {
+                                const float2 o = *at;
+                                v.x += o.x;
+                                v.y += o.y;
+                            }
+                            *at = v;
+                        }
+                }
+                __syncthreads();
+            }
+            piece += PIECE;
+        } while (piece < kc1);
         for (int e = tid; e < 16 * R; e += FEW_THREADS) {
             float s = 0.f;
 #pragma unroll
