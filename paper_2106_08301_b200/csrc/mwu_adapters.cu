@@ -246,19 +246,16 @@ __device__ __forceinline__ void keep8(uint4 &v, int valid) {
     v.z = keep_valid(v.z, 4, valid);
     v.w = keep_valid(v.w, 6, valid);
 }
-// The next bf16 term of s, and s without it.  An infinity leaves nothing (inf - inf would make NaN of it), and what would round to an
-// infinity without being one goes to the largest bf16 (its remainder is below 2^120).
-__device__ __forceinline__ float next_term(float &s) {
-    float h = __bfloat162float(__float2bfloat16_rn(s));
-    if (isinf(h)) {
-        if (isinf(s)) {
-            s = 0.f;
-            return h;
-        }
-        h = copysignf(0x1.fep127f, h);
-    }
-    s -= h;
-    return h;
+// The next bf16 terms of two numbers, and the numbers without them.  All terms but the last stop at the largest bf16: a number that would
+// round to an infinity keeps a finite remainder, and an infinity goes whole into the last term (inf - inf would make NaN of it).
+template <bool LAST>
+__device__ __forceinline__ unsigned next_terms(float &lo, float &hi) {
+    unsigned w;
+    if (LAST) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    lo -= __uint_as_float(w << 16);
+    hi -= __uint_as_float(w & 0xffff0000u);
+    return w;
 }
 __device__ __forceinline__ float remote_f32(unsigned local, unsigned cta) {
     unsigned at;
@@ -452,13 +449,14 @@ mwu_adapters_few_kernel(const Params p) {
         // ---- the cluster's sum, scaled, as bf16 terms ----
         const float scale = p.scale ? __ldg(p.scale + a) : 1.f;
         for (int e = tid; e < 16 * R; e += FEW_THREADS) {
-            float s = 0.f;
+            float s = 0.f, none = 0.f;
 #pragma unroll 4
             for (int o = 0; o < ctas; ++o) s += remote_f32(smem_u32(&(&sm->part[0][0])[e]), (unsigned)o);
             s *= scale;
             if (e % R >= p.rank) s = 0.f;                   // (an infinity of X times the zeros that stand for A there is NaN)
 #pragma unroll
-            for (int q = 0; q < TERMS; ++q) sm->T[q][e / R][e % R] = __float2bfloat16_rn(next_term(s));
+            for (int q = 0; q < TERMS; ++q)
+                reinterpret_cast<unsigned short &>(sm->T[q][e / R][e % R]) = (unsigned short)(q + 1 < TERMS ? next_terms<false>(s, none) : next_terms<true>(s, none));
         }
         cluster_arrive();                                   // the others' sums have been read; waited for below
         __syncthreads();
@@ -862,11 +860,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                 for (int q = 0; q < C::TERMS; ++q) {
                     unsigned w[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float lo = next_term(f[2 * j]), hi = next_term(f[2 * j + 1]);
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                        w[j] = *reinterpret_cast<const unsigned *>(&h);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = q + 1 < C::TERMS ? next_terms<false>(f[2 * j], f[2 * j + 1]) : next_terms<true>(f[2 * j], f[2 * j + 1]);
 #pragma unroll 1
                     for (int o = o0; o < o1; ++o) {
                         unsigned at;
