@@ -964,20 +964,38 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                         *at = y;
                     }
                     // Whole boxes, clipped at the last column by the map, which clips a store at 16 bytes only.
-                    if (rows_here == 32 && (n0 + C::CW <= p.rows || p.rows % (C::CW / 8) == 0)) {
-                        fence_proxy_async();
-                        __syncwarp();
+                    // (The fence is for all ways out: the store, and the slot's next load, come behind what the lanes wrote.)
+                    fence_proxy_async();
+                    __syncwarp();
+                    constexpr int unit = C::CW / 8;
+                    const int r0 = lane >> 3, g = lane & 7;
+                    const long long first_at = (long long)(row0 + quarter * 32 + r0) * p.ldy + n0 + g * unit;
+                    if (rows_here == 32 && (n0 + C::CW <= p.rows || p.rows % unit == 0)) {
                         if (lane == 0) {
                             tma_store_2d(&tm_y, smem_u32(box), n0, row0 + quarter * 32);
+                            bulk_commit();
+                            bulk_wait_read();                   // (a slot given back a chunk later, unread stores or not: 54 us instead of 50)
                         }
-                    } else {                                    // the rows behind are another segment's, the columns behind the caller's
-                        __syncwarp();
+                    } else if (n0 + C::CW <= p.rows) {          // the rows behind are another segment's
+                        unsigned char *to = reinterpret_cast<unsigned char *>(p.Y) + first_at * (F32 ? 4 : 2);
+#pragma unroll 1
+                        for (int b = r0; b < rows_here; b += 8, to += 8 * p.ldy * (F32 ? 4 : 2)) {
+                            uint4 y[2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (b + 4 * i < rows_here) y[i] = *reinterpret_cast<const uint4 *>(box + (b + 4 * i) * 128 + ((g ^ ((b + 4 * i) & 7)) << 4));
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (b + 4 * i < rows_here) *reinterpret_cast<uint4 *>(to + 4 * i * p.ldy * (F32 ? 4 : 2)) = y[i];
+                        }
+                    } else {                                    // and the columns behind are the caller's
+                        const int left = p.rows - n0 - g * unit;
                         for (int b = 0; b < rows_here; b += 4) {
-                            const int r = b + (lane >> 3), g = lane & 7, left = p.rows - n0 - g * (C::CW / 8);
+                            const int r = b + r0;
                             if (r < rows_here && left > 0) {
                                 const uint4 y = *reinterpret_cast<const uint4 *>(box + r * 128 + ((g ^ (r & 7)) << 4));
-                                const long long at = (long long)(row0 + quarter * 32 + r) * p.ldy + n0 + g * (C::CW / 8);
-                                if (left >= C::CW / 8) {
+                                const long long at = first_at + b * p.ldy;
+                                if (left >= unit) {
                                     *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.Y) + at * (F32 ? 4 : 2)) = y;
                                 } else {
                                     const unsigned w[4] = {y.x, y.y, y.z, y.w};
@@ -993,12 +1011,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                         }
                     }
                 }
-                if (lane == 0) {
-                    bulk_commit();
-                    bulk_wait_read();                       // (a slot given back a chunk later, unread stores or not: 54 us instead of 50)
-                    mbar_arrive(smem_u32(&sm->empty[s]));
-                }
-                __syncwarp();
+                __syncwarp();                                   // all lanes have read the box before it is given back
+                if (lane == 0) mbar_arrive(smem_u32(&sm->empty[s]));
             }
             // on to the first slot behind this item's chunks
             if (half) {
