@@ -452,6 +452,11 @@ int mwu_conv_dense(int64_t rows, const void *Wd, int64_t ldw, const void *X_nchw
  * not meant for production code.
  */
 void mwu_debug_conv_wait(int64_t limit_cycles, int64_t withhold_stage);
+/*
+ * mwu_debug_rows_wait -- the same for the grouped products and for the kernel for many rows of mwu_adapters_add, read when they are
+ * called; `slot` names a slot of the pipeline's ring that never counts as filled, in every CTA (-1: none).
+ */
+void mwu_debug_rows_wait(int64_t limit_cycles, int64_t slot);
 
 #ifdef __cplusplus
 }

@@ -21,7 +21,7 @@ EXPORTS = ["mwu_status_string", "mwu_kernel_launches", "mwu_count_from_permille"
            "mwu_gemm_ws", "mwu_conv_implicit", "mwu_conv_workspace_bytes", "mwu_conv_implicit_ws",
            "mwu_debug_conv_wait", "mwu_keep_n_of_m", "mwu_gemm_dense", "mwu_conv_dense_workspace_bytes",
            "mwu_conv_dense", "mwu_gemm_grouped", "mwu_gemm_grouped_dx", "mwu_gemm_grouped_dw",
-           "mwu_adapters_add"]
+           "mwu_adapters_add", "mwu_debug_rows_wait"]
 MWU_MAX_GROUPS = 1024
 MWU_MAX_GROUPED_SIDE = 1048576
 MWU_MAX_RANK = 128
@@ -115,8 +115,9 @@ def lib() -> ctypes.CDLL:
         L.mwu_gemm_grouped_dw.argtypes = [i64] * 3 + [vp, vp, i64, i64, vp, i64, vp, i64, i64, i32, i32, vp, vp]
         L.mwu_adapters_add.restype = ctypes.c_int
         L.mwu_adapters_add.argtypes = ([i64] * 4 + [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, vp, vp, i64, i32, vp, vp])
-        L.mwu_debug_conv_wait.restype = None
-        L.mwu_debug_conv_wait.argtypes = [i64, i64]
+        for fn in (L.mwu_debug_conv_wait, L.mwu_debug_rows_wait):
+            fn.restype = None
+            fn.argtypes = [i64, i64]
         _lib = L
     return _lib
 
@@ -362,6 +363,10 @@ def mwu_adapters_add(adapters, rank, rows, cols, A, lda, a_stride, Bm, ldb, b_st
 
 def mwu_debug_conv_wait(limit_cycles: int, withhold_stage: int) -> None:
     lib().mwu_debug_conv_wait(int(limit_cycles), int(withhold_stage))
+
+
+def mwu_debug_rows_wait(limit_cycles: int, slot: int) -> None:
+    lib().mwu_debug_rows_wait(int(limit_cycles), int(slot))
 
 
 def mwu_conv_workspace_bytes(desc, n, c, h, w, kh, kw, stride, pad) -> int:

@@ -50,6 +50,7 @@ struct Params {
     int few_rows;                       // FEW_ROWS, or as many as may be
     int sorted;                         // the few-rows kernel's rows are sorted by adapter
     int beside;                         // the few-rows kernel runs beside the tile kernel launched before it
+    WaitLimits wait;                    // of the tile kernel
     unsigned *dev_status;
 };
 
@@ -645,7 +646,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < TILE_SLOTS; ++s) {
-            mbar_init(smem_u32(&sm->full[s]), 1);
+            mbar_init(smem_u32(&sm->full[s]), 1 + (s == p.wait.dead_slot));
             mbar_init(smem_u32(&sm->empty[s]), 4);          // the four warps of a chunk; a stage's MMAs arrive for all four
         }
         for (int b = 0; b < 2; ++b) {
@@ -693,7 +694,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             if (a < 0) continue;
             cluster_arrive();
             for (int ks = ks0; ok && ks < ks1; ++ks) {
-                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort);
+                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 if (elect_one()) {
                     const unsigned bar = smem_u32(&sm->full[at.slot]), dst = smem_u32(ring + at.slot * C::SLOT);
@@ -714,7 +715,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
                     cluster_wait();                         // (3)
                     waited = true;
                 }
-                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort);
+                if (at.round) ok = warp_wait_spin(smem_u32(&sm->empty[at.slot]), (at.round & 1u) ^ 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 if (elect_one()) {
                     const unsigned bar = smem_u32(&sm->full[at.slot]), dst = smem_u32(ring + at.slot * C::SLOT);
@@ -737,7 +738,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
         if (__any_sync(0xffffffffu, *abort)) {
             for (int s = 0; s < slots; ++s)
                 if (at.round || s < at.slot)                // this slot's latest load
-                    mbar_wait(smem_u32(&sm->full[s]), (s < at.slot ? at.round : at.round - 1u) & 1u, &sm->drain_abort);
+                    mbar_wait(smem_u32(&sm->full[s]), (s < at.slot ? at.round : at.round - 1u) & 1u, &sm->drain_abort, p.wait.cycles);
             __syncwarp();
         }
     } else if (warp == 1) {
@@ -750,13 +751,13 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             if (sm->adapter[it] < 0) continue;
             cluster_arrive();
             for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
-                ok = warp_wait_spin(smem_u32(&sm->tempty1[use & 1u]), ((use >> 1) & 1u) ^ 1u, abort);
+                ok = warp_wait_spin(smem_u32(&sm->tempty1[use & 1u]), ((use >> 1) & 1u) ^ 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 tc_fence_after();
                 const int k1 = min(ks1, k0 + PIECE);
                 for (int ks = k0; ks < k1; ++ks, at.advance(1, slots)) {
                     const int s = at.slot;
-                    ok = warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort);
+                    ok = warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort, p.wait.cycles);
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -783,8 +784,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
             for (int j = 0; ok && j < nc1 - nc0; ++j, at.advance(1, slots)) {
                 const int s = at.slot;
                 const unsigned buf = (unsigned)j & 1u;
-                ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((used2 >> buf) & 1u) ^ 1u, abort) &&
-                     warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort);
+                ok = warp_wait_spin(smem_u32(&sm->tempty2[buf]), ((used2 >> buf) & 1u) ^ 1u, abort, p.wait.cycles) &&
+                     warp_wait_spin(smem_u32(&sm->full[s]), at.round & 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 used2 ^= 1u << buf;
                 tc_fence_after();
@@ -807,7 +808,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
         // everything this thread issued must have retired before tensor memory is freed
         if (elect_one()) umma_commit(smem_u32(&sm->drain));
         __syncwarp();
-        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort);
+        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort, p.wait.cycles);
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane, tid = threadIdx.x - 64;
@@ -832,7 +833,7 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
 #pragma unroll
             for (int j = 0; j < MINE; ++j) t[j] = 0.f;
             for (int k0 = ks0; ok && k0 < ks1; k0 += PIECE, ++use) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull1[use & 1u]), (use >> 1) & 1u, abort));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull1[use & 1u]), (use >> 1) & 1u, abort, p.wait.cycles));
                 if (!ok) break;
                 tc_fence_after();
                 if (has_t) {
@@ -925,8 +926,8 @@ mwu_adapters_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_
 #pragma unroll 1
             for (int j = half; ok && j < nc1 - nc0; j += 2, ++used2, at.advance(2, slots)) {
                 const int i = nc0 + j, s = at.slot;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), used2 & 1u, abort) &&
-                                                 mbar_wait(smem_u32(&sm->full[s]), at.round & 1u, abort));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull2[half]), used2 & 1u, abort, p.wait.cycles) &&
+                                                 mbar_wait(smem_u32(&sm->full[s]), at.round & 1u, abort, p.wait.cycles));
                 if (!ok) break;
                 tc_fence_after();
                 unsigned v[C::CW / 32][32];
@@ -1186,6 +1187,7 @@ extern "C" int mwu_adapters_add(int64_t adapters, int64_t rank, int64_t rows, in
     p.scale = scale; p.offsets = offsets; p.which = which; p.Y0 = Y0; p.Y = Y;
     p.adapters = (int)adapters; p.rank = (int)rank; p.rows = (int)rows; p.cols = (int)cols; p.segments = (int)segments; p.M = (int)M;
     p.dev_status = dev_status;
+    p.wait = gemm::wait_limits();
     return y_dtype ? adapters::launch_rank<true>(p, sm_count, (cudaStream_t)cuda_stream)
                    : adapters::launch_rank<false>(p, sm_count, (cudaStream_t)cuda_stream);
 }

@@ -66,6 +66,7 @@ struct GroupedParams {
     int feature_side, block_bytes;      // of 64 reduction steps: bytes of features, of all
     int blocks, stages;                 // blocks of a stage, stages of the ring
     int out_fp32, accumulate;
+    WaitLimits wait;
     unsigned *dev_status;
 };
 
@@ -113,7 +114,7 @@ __device__ __forceinline__ unsigned long long make_desc_mn(unsigned smem_addr) {
     return d;
 }
 // a wait that also orders what another CTA of the cluster wrote before it arrived
-__device__ __forceinline__ bool mbar_wait_cluster(unsigned bar, unsigned parity, volatile int *abort) {
+__device__ __forceinline__ bool mbar_wait_cluster(unsigned bar, unsigned parity, volatile int *abort, long long limit) {
     const long long t0 = clock64();
 #pragma unroll 1
     while (true) {
@@ -125,7 +126,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(unsigned bar, unsigned parity,
             : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
         if (*abort) return false;
-        if (clock64() - t0 > WAIT_LIMIT_CYCLES) { *abort = 1; return false; }
+        if (clock64() - t0 > limit) { *abort = 1; return false; }
     }
 }
 
@@ -202,9 +203,9 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(smem_u32(&sm->full[s]), 1);
+            mbar_init(smem_u32(&sm->full[s]), 1 + (s == p.wait.dead_slot));
             mbar_init(smem_u32(&sm->empty[s]), 1);
-            mbar_init(smem_u32(&sm->tail[s]), 1);
+            mbar_init(smem_u32(&sm->tail[s]), 1 + (s == p.wait.dead_slot));
             mbar_init(smem_u32(&sm->peer_fixed[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -281,7 +282,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
             const unsigned line_bytes = OP == G_DW ? (unsigned)boxes * G_SUB : (unsigned)boxed * 128u;
             const unsigned mine = feature_bytes<OP>(p, f0), pair_bytes = feature_bytes<OP>(p, t.feature0) + feature_bytes<OP>(p, t.feature0 + 128) + 2 * line_bytes;
             for (int b0 = 0; b0 < n_blk; b0 += BL) {
-                ok = warp_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort);
+                ok = warp_wait_spin(smem_u32(&sm->empty[stage]), phase ^ 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 const int nb = min(BL, n_blk - b0), last = t.red_len - (b0 + nb - 1) * 64;     // reduction steps from the last block on
                 const bool tail = OP == G_DW && last < 64 && (last & 15);
@@ -333,8 +334,8 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         if (__any_sync(0xffffffffu, *abort)) {
             volatile int *drain_abort = &sm->drain_abort;
             if (rank == 0)
-                for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->full[s]), s < stage ? phase : phase ^ 1u, drain_abort);
-            for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->tail[s]), ((tails >> s) & 1u) ^ 1u, drain_abort);
+                for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->full[s]), s < stage ? phase : phase ^ 1u, drain_abort, p.wait.cycles);
+            for (int s = 0; s < p.stages; ++s) mbar_wait(smem_u32(&sm->tail[s]), ((tails >> s) & 1u) ^ 1u, drain_abort, p.wait.cycles);
             __syncwarp();
         }
     } else if (warp == 1 && rank == 0) {
@@ -342,23 +343,25 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         int stage = 0;
         unsigned phase = 0, use = 0;
         bool ok = true;
+        const bool leader = elect_one();                    // the lane that issues
         for (unsigned k = pair; ok && k < total; k += n_pairs) {
             grouped_tile<OP>(p, sm, k, f_tiles, t);
             const int red_len = __shfl_sync(0xffffffffu, t.red_len, 0), n_blk = (red_len + 63) / 64, chunk = p.out_fp32 ? G_CHUNK : G_CHUNK_BF16;
             const unsigned idesc = make_idesc_pair(__shfl_sync(0xffffffffu, t.line_pad, 0)) | (OP != G_FORWARD ? 1u << 15 : 0u) | (OP == G_DW ? 1u << 16 : 0u);
             for (int c0 = 0; ok && c0 < n_blk; c0 += chunk, ++use) {
                 const unsigned buf = use & 1u;
-                ok = warp_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort);
+                ok = warp_wait_spin(smem_u32(&sm->tempty[buf]), ((use >> 1) & 1u) ^ 1u, abort, p.wait.cycles);
                 if (!ok) break;
                 tc_fence_after();
                 const int c1 = min(n_blk, c0 + chunk);
                 for (int b0 = c0; b0 < c1; b0 += BL) {
-                    // (no vote and no warp barrier: every lane looks at the same barriers and decides alike)
-                    if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort)) { ok = false; break; }
+                    // (No vote, no election and no warp barrier in this loop: where the limit runs out lanes may leave it at different
+                    // stages, and the vote behind it is the first place where they need one another again.)
+                    if (!mbar_wait_spin(smem_u32(&sm->full[stage]), phase, abort, p.wait.cycles)) { ok = false; break; }
                     tc_fence_after();
                     const int nb = min(BL, n_blk - b0);
                     unsigned af = smem_u32(ring) + (unsigned)(stage * BL * p.block_bytes);
-                    if (elect_one()) {
+                    if (leader) {
                         for (int b = b0; b < b0 + nb; ++b, af += (unsigned)p.block_bytes) {
                             const unsigned al = af + (unsigned)p.feature_side;
                             const unsigned long long fdesc = OP == G_FORWARD ? make_desc(af) : make_desc_mn(af);
@@ -376,14 +379,14 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (elect_one()) umma2_commit_both(smem_u32(&sm->tfull[buf]));
+                if (leader) umma2_commit_both(smem_u32(&sm->tfull[buf]));
                 __syncwarp();
             }
         }
         // everything this thread issued must have retired before tensor memory is freed
-        if (elect_one()) umma2_commit_local(smem_u32(&sm->drain));
+        if (leader) umma2_commit_local(smem_u32(&sm->drain));
         __syncwarp();
-        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort);
+        mbar_wait(smem_u32(&sm->drain), 0, &sm->drain_abort, p.wait.cycles);
         __syncwarp();
     } else if (warp == G_FIX_WARP) {
         // ---------------- foreign rows of a group's last stage ----------------
@@ -396,7 +399,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 const int rem = t.red_len & 63;
                 if (rem & 15) {
                     const unsigned stage = (pos + n_st - 1) % (unsigned)p.stages;
-                    ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort);
+                    ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort, p.wait.cycles);
                     if (!ok) break;
                     // rows rem .. of the next multiple of 16, 128 bytes each, in the sub-tiles of either operand
                     const int rows = 16 - (rem & 15);
@@ -410,7 +413,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                     if (rank) {
                         if (lane == 0) mbar_arrive_cluster(smem_u32(&sm->peer_fixed[stage]), 0);
                     } else {
-                        ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&sm->peer_fixed[stage]), (tails >> stage) & 1u, abort));
+                        ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&sm->peer_fixed[stage]), (tails >> stage) & 1u, abort, p.wait.cycles));
                         if (!ok) break;
                         fence_proxy_async();
                         if (lane == 0) mbar_arrive(smem_u32(&sm->full[stage]));
@@ -457,7 +460,7 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
                 for (int j = 0; j < 32; ++j) acc[q][j] = 0.f;
             for (int c0 = 0; c0 < n_st; c0 += chunk, ++use) {
                 const unsigned buf = use & 1u;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull[buf]), (use >> 1) & 1u, abort));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sm->tfull[buf]), (use >> 1) & 1u, abort, p.wait.cycles));
                 if (!ok) break;
                 tc_fence_after();
                 const unsigned trow = tmem_base + ((unsigned)(quarter * 32) << 16) + buf * 256u + (unsigned)(odd * 32);
@@ -539,6 +542,15 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         tc_fence_after();
         tmem_dealloc2(tmem_base, 512);
     }
+}
+
+// testing aid (see mwu.h)
+static std::atomic<long long> g_rows_limit{WAIT_LIMIT_CYCLES};
+static std::atomic<int> g_rows_dead_slot{-1};
+WaitLimits wait_limits() { return {g_rows_limit.load(std::memory_order_relaxed), g_rows_dead_slot.load(std::memory_order_relaxed)}; }
+static void set_wait_limits(long long cycles, long long slot) {
+    g_rows_limit.store(cycles > 0 ? cycles : WAIT_LIMIT_CYCLES, std::memory_order_relaxed);
+    g_rows_dead_slot.store(slot >= 0 && slot < G_MOST_STAGES ? (int)slot : -1, std::memory_order_relaxed);
 }
 
 template <int OP, int BL>
@@ -637,6 +649,7 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
     p.groups = (int)groups; p.M = (int)M; p.features = (int)features; p.reduction = (int)red;
     p.feature_box = features <= 32 ? 32 : features <= 64 ? 64 : 128;
     p.dev_status = dev_status;
+    p.wait = wait_limits();
     const int64_t f_tiles = (features + 255) / 256;
     if ((M / 32 + (M < groups ? M : groups)) * f_tiles >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
     int sm_count = 0;
@@ -664,6 +677,8 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
 
 }  // namespace gemm
 }  // namespace mwu
+
+extern "C" void mwu_debug_rows_wait(int64_t limit_cycles, int64_t slot) { mwu::gemm::set_wait_limits(limit_cycles, slot); }
 
 extern "C" int mwu_gemm_grouped(int64_t groups, int64_t rows, int64_t cols, const void *Wd, int64_t ldw, int64_t w_stride,
                                 const int32_t *offsets, const void *X, int64_t M, int64_t ldx, void *Y, int64_t ldy, int32_t y_dtype,
@@ -698,6 +713,7 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     p.out = dW; p.ldo = lddw; p.out_stride = dw_stride; p.out_fp32 = dw_dtype; p.accumulate = accumulate;
     p.groups = (int)groups; p.M = (int)M; p.features = (int)cols; p.lines = (int)rows;
     p.dev_status = dev_status;
+    p.wait = wait_limits();
     if (groups * ((rows + 63) / 64) * ((cols + 255) / 256) >= (int64_t(1) << 30)) return MWU_ERR_SHAPE;
     int sm_count = 0;
     const int rc = check_device(&sm_count);

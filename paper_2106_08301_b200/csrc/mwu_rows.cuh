@@ -6,6 +6,14 @@
 namespace mwu {
 namespace gemm {
 
+// Limit of the bounded waits in cycles, and (testing aid, mwu_debug_rows_wait) a slot of the ring whose barrier waits for one arrival more
+// than it gets; none: -1.  (Left to the barriers' set-up, since a test a stage in the producer's loop costs up to 5 % of a product.)
+struct WaitLimits {
+    long long cycles;
+    int dead_slot;
+};
+WaitLimits wait_limits();               // mwu_grouped.cu
+
 // the two halves of a cluster barrier, for what can be done between them
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
