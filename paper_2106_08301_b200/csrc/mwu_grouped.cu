@@ -392,15 +392,18 @@ mwu_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_f, const __grid
         // ---------------- foreign rows of a group's last stage ----------------
         if (OP == G_DW) {
             unsigned pos = 0, tails = 0;                    // pos: place of the tile's first stage in the ring; tails as in the producer
+            long long behind = 0;                           // stages since the last one handed on: the limit is for each of them
             bool ok = true;
             for (unsigned k = pair; ok && k < total; k += n_pairs) {
                 grouped_tile<OP>(p, sm, k, f_tiles, t);
                 const unsigned n_blk = (unsigned)(t.red_len + 63) / 64, n_st = (n_blk + (unsigned)BL - 1) / (unsigned)BL;
                 const int rem = t.red_len & 63;
+                behind += n_st;
                 if (rem & 15) {
                     const unsigned stage = (pos + n_st - 1) % (unsigned)p.stages;
-                    ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort, p.wait.cycles);
+                    ok = warp_wait_spin(smem_u32(&sm->tail[stage]), (tails >> stage) & 1u, abort, p.wait.cycles * behind);
                     if (!ok) break;
+                    behind = 0;
                     // rows rem .. of the next multiple of 16, 128 bytes each, in the sub-tiles of either operand
                     const int rows = 16 - (rem & 15);
                     unsigned char *block = ring + (stage * (unsigned)BL + (n_blk - 1) % (unsigned)BL) * (unsigned)p.block_bytes;

@@ -86,3 +86,18 @@ def test_a_limit_that_nothing_reaches_changes_nothing():
     with waits(LIMIT, 1000):
         b.run(b.Y0, Z)
     assert int(b.st.item()) == 0 and torch.equal(Y, Z)
+
+
+@pytest.mark.parametrize("lengths", [[(1 << 22) + 5], [1 << 22] + [16] * 73 + [13], [13] + [16] * 146 + [1 << 22, 5]], ids=lambda x: f"{len(x)} groups")
+def test_a_group_may_take_longer_than_a_wait(lengths):
+    """The limit is for one stage: a gradient of 4194304 rows takes 20 ms, several times the 2.5 ms set here, and the warp that zeroes
+    foreign rows waits all through it, or through the tiles before its own."""
+    gen, at, n = gen_of(12), offsets_of(lengths), len(lengths)
+    m, off = at[-1], torch.tensor(at, dtype=torch.int32, device="cuda")
+    dY, X, dW, st = normal(gen, m, 8), normal(gen, m, 8), torch.zeros(n, 8, 8, device="cuda"), new_status()
+    with waits(5_000_000):
+        B.mwu_gemm_grouped_dw(n, 8, 8, off, dY, m, 8, X, 8, dW, 8, 64, 1, 0, st)
+    assert int(st.item()) == 0
+    for g in range(n):
+        d, x = dY[at[g]:at[g + 1]].to(F64).t(), X[at[g]:at[g + 1]].to(F64)
+        check(dW[g], d @ x, d.abs() @ x.abs(), lengths[g], 1)
