@@ -120,12 +120,13 @@ __device__ __forceinline__ void find_item(const Params &p, Finder *f, int per, i
 // Up to SORTED_ROWS rows of a call are worked on adapter by adapter, 16 rows at a time, wherever in the batch they are: 64 tokens of 32
 // adapters read every adapter once, not twice (4096 -> 16384: 17 us instead of 35), and 512 tokens of 4 adapters once for 16 rows.
 struct Sorter {
-    int key[SORTED_ROWS];               // adapter of a row; NOBODY: not this kernel's
+    alignas(16) int key[SORTED_ROWS];   // adapter of a row; NOBODY: not this kernel's (read 16 bytes at a time)
     int row[SORTED_ROWS];               // rows in the order of their adapters
     int start[SORTED_ROWS + 1];         // where an item's rows start in `row`
     unsigned starts[SORTED_ROWS / 32];
     int counted;
 };
+static_assert(alignof(Sorter) == 16 && SORTED_ROWS % 4 == 0, "adapters: keys are read in fours");
 constexpr int NOBODY = 0x7fffffff;
 
 // Returns the number of items, -1 where the list makes no sense.  All threads of the CTA, each placing two rows by counting those that
