@@ -373,7 +373,7 @@ int mwu_gemm_dense(int64_t rows, int64_t cols, const void *Wd, int64_t ldw, cons
  *                    gets zeros.  accumulate 1 (fp32 only): added to what dW holds, groups without rows left alone.
  * 1 <= groups <= MWU_MAX_GROUPS; rows, cols <= MWU_MAX_GROUPED_SIDE, of any value, not only multiples of something.
  * Leading dimensions and group strides are multiples of 8 elements (fp32 outputs: of 4).  M == 0 is a no-op for the first two; the
- * third then still writes its zeros.  Outputs must not overlap inputs.
+ * third then still writes its zeros; X, Y, dY and dX may then be NULL.  Outputs must not overlap inputs.
  * Products are bf16 x bf16 accumulated in fp32; fp32 results are summed in pieces of 512 products, so that what the
  * tensor core drops of a long sum stays below 1e-6 of it, bf16 results in pieces of 262144.  The same call on the same inputs
  * gives the same bits.
@@ -409,7 +409,7 @@ int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, const int32_
  *   Y0           in   its output, [M][ldy >= rows], of Y's type; may be Y itself (added in place) or NULL (zeros), and must not
  *                     overlap Y otherwise
  *   Y            out  [M][ldy]; y_dtype 0: bf16, 1: fp32.  Rows of no segment are left as they are.
- * M == 0 or segments == 0 is a no-op.  1 <= rank <= MWU_MAX_RANK, segments <= MWU_MAX_SEGMENTS, rows and cols <= MWU_MAX_GROUPED_SIDE, of any value; lda, ldb, ldx, a_stride,
+ * M == 0 or segments == 0 is a no-op (X, Y and Y0, or `which`, may then be NULL).  1 <= rank <= MWU_MAX_RANK, segments <= MWU_MAX_SEGMENTS, rows and cols <= MWU_MAX_GROUPED_SIDE, of any value; lda, ldb, ldx, a_stride,
  * b_stride and a bf16 ldy are multiples of 8 elements, an fp32 ldy of 4.  X A^T is held in fp32 and enters the second product as
  * bf16 terms (two for a bf16 Y, three for fp32), so no rounding but Y's own shows.  An infinity in X A^T gives what the formula
  * gives; one in B makes the row's result at that column an infinity or NaN, since a term of X A^T may be zero.  The same call on the same

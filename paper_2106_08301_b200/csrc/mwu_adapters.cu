@@ -1167,7 +1167,8 @@ extern "C" int mwu_adapters_add(int64_t adapters, int64_t rank, int64_t rows, in
                                 const int32_t *offsets, const int32_t *which, const void *X, int64_t M, int64_t ldx, const void *Y0,
                                 void *Y, int64_t ldy, int32_t y_dtype, uint32_t *dev_status, void *cuda_stream) {
     using namespace mwu;
-    if (!A || !B || !offsets || !which || !X || !Y || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if (!A || !B || !offsets || !dev_status || M < 0 || (segments > 0 && !which) || (M > 0 && (!X || !Y)))      // (an empty tensor has no address)
+        return MWU_ERR_INVALID_ARG;
     if (y_dtype != 0 && y_dtype != 1) return MWU_ERR_INVALID_ARG;
     if (adapters <= 0 || adapters >= (int64_t(1) << 31) || segments < 0 || segments > MWU_MAX_SEGMENTS) return MWU_ERR_SHAPE;
     if (rank <= 0 || rank > MWU_MAX_RANK || rows <= 0 || cols <= 0 || lda < cols || ldb < rank || ldx < cols || ldy < rows) return MWU_ERR_SHAPE;

@@ -637,7 +637,7 @@ static int run_lines(int64_t groups, int64_t rows, int64_t cols, const void *Wd,
                      const void *in, int64_t M, int64_t ldi, void *out, int64_t ldo, int32_t out_dtype, uint32_t *dev_status,
                      void *cuda_stream) {
     const int64_t features = OP == G_FORWARD ? rows : cols, red = OP == G_FORWARD ? cols : rows;
-    if (!Wd || !offsets || !in || !out || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if (!Wd || !offsets || !dev_status || M < 0 || (M > 0 && (!in || !out))) return MWU_ERR_INVALID_ARG;    // (an empty tensor has no address)
     if (out_dtype != 0 && out_dtype != 1) return MWU_ERR_INVALID_ARG;
     if (groups <= 0 || groups > MWU_MAX_GROUPS || rows <= 0 || cols <= 0 || ldw < cols || ldi < red || ldo < features) return MWU_ERR_SHAPE;
     if (rows > MWU_MAX_GROUPED_SIDE || cols > MWU_MAX_GROUPED_SIDE || M >= (int64_t(1) << 31) - 256) return MWU_ERR_SHAPE;
@@ -702,7 +702,7 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
                                    int32_t dw_dtype, int32_t accumulate, uint32_t *dev_status, void *cuda_stream) {
     using namespace mwu;
     using namespace mwu::gemm;
-    if (!offsets || !dY || !X || !dW || !dev_status || M < 0) return MWU_ERR_INVALID_ARG;
+    if (!offsets || !dW || !dev_status || M < 0 || (M > 0 && (!dY || !X))) return MWU_ERR_INVALID_ARG;      // (an empty tensor has no address)
     if ((dw_dtype != 0 && dw_dtype != 1) || (accumulate != 0 && accumulate != 1) || (accumulate && !dw_dtype)) return MWU_ERR_INVALID_ARG;
     if (groups <= 0 || groups > MWU_MAX_GROUPS || rows <= 0 || cols <= 0 || lddy < rows || ldx < cols || lddw < cols) return MWU_ERR_SHAPE;
     if (rows > MWU_MAX_GROUPED_SIDE || cols > MWU_MAX_GROUPED_SIDE || M >= (int64_t(1) << 31) - 256) return MWU_ERR_SHAPE;
@@ -729,6 +729,7 @@ extern "C" int mwu_gemm_grouped_dw(int64_t groups, int64_t rows, int64_t cols, c
     CUtensorMap tmap_f;
     LineMaps maps_l;
     const int64_t m_rows = M > 0 ? M : 1;               // no rows: the maps are never used, the gradients are zeros
+    if (M == 0) X = dY = dW;                            // (a map has to name some address)
     if (!encode_bf16(encode, &tmap_f, X, cols, m_rows, ldx, 64, 0, 0) || !encode_bf16(encode, &maps_l.m[0], dY, rows, m_rows, lddy, 64, 0, 0))
         return MWU_ERR_CUDA;
     maps_l.m[1] = maps_l.m[2] = maps_l.m[0];
