@@ -152,13 +152,17 @@ _numel, _is_contiguous, _device_of, _data_ptr = (torch.Tensor.numel, torch.Tenso
 
 
 def _address(t: Optional[torch.Tensor], dtype, device: int, reach: int):
-    """The address of a contiguous tensor of this type on this device with at least `reach` elements, or None: a kernel reads what it is
-    given as its own type, as far as its sizes say."""
+    """The address of a tensor of this type on this device with at least `reach` elements from its first on, or None: a kernel reads what
+    it is given as its own type, as far as its sizes say.  Contiguous, or a view whose rows are (X[:, :k] of a wider buffer, whose
+    leading dimension the call then names)."""
     if t is None:
         return None
     if t.dtype is dtype and _numel(t) >= reach and _is_contiguous(t) and _device_of(t) == device:
         return _data_ptr(t)
-    raise ValueError(f"contiguous {dtype} tensors of the current device, of at least {reach} elements here: "
+    if t.dtype is dtype and _device_of(t) == device and t.dim() > 1 and t.stride(-1) == 1 and \
+            1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) >= reach:
+        return _data_ptr(t)
+    raise ValueError(f"{dtype} tensors of the current device with contiguous rows, of at least {reach} elements here: "
                      f"got {t.dtype} on {t.device} of shape {tuple(t.shape)}, strides {t.stride()}")
 
 

@@ -67,3 +67,23 @@ def test_sizes_beyond_the_tensors_are_refused(name, change):
 def test_no_rows_reach_nothing():
     assert B.mwu_gemm_grouped(**{**PRODUCT, "M": 0, "X": new(0, K), "Y": new(0, N, dtype=F32)}) == B.MWU_OK
     assert B.mwu_adapters_add(**{**ADAPTERS, "M": 0, "X": new(0, K), "Y": new(0, N), "Y0": None, "scale": None}) == B.MWU_OK
+
+
+def wide(*shape, dtype=BF16, more=8):
+    """A view of the first columns of a wider buffer."""
+    return new(*shape[:-1], shape[-1] + more, dtype=dtype)[..., :shape[-1]]
+
+
+def test_views_with_contiguous_rows_are_taken():
+    assert B.mwu_gemm_grouped(**{**PRODUCT, "Wd": wide(G, N, K), "ldw": K + 8, "w_stride": N * (K + 8), "X": wide(M, K), "ldx": K + 8,
+                                 "Y": wide(M, N, dtype=F32), "ldy": N + 8}) == B.MWU_OK
+    assert B.mwu_gemm_grouped_dw(**{**DW, "dW": new(G, 2, N, K, dtype=F32)[:, 1], "dw_stride": 2 * N * K, "dY": wide(M, N), "lddy": N + 8}) == B.MWU_OK
+    assert B.mwu_adapters_add(**{**ADAPTERS, "X": wide(M, K), "ldx": K + 8, "Y": wide(M, N), "Y0": None, "ldy": N + 8}) == B.MWU_OK
+
+
+@pytest.mark.parametrize("change", [dict(X=wide(M, K)[:-1], ldx=K + 8), dict(X=wide(M, K), ldx=K + 16), dict(X=new(K, M).t()),
+                                    dict(X=new(1, K).expand(M, K)), dict(X=new(M, 2 * K)[:, ::2], ldx=2 * K), dict(offsets=new(2 * G + 2, dtype=I32)[::2]),
+                                    dict(X=wide(M, K, dtype=F32), ldx=K + 8), dict(Y=new(N, M, dtype=F32).t())])
+def test_other_views_are_refused(change):
+    with pytest.raises(ValueError):
+        B.mwu_gemm_grouped(**{**PRODUCT, **change})
