@@ -2,22 +2,24 @@
 //
 //   Y[m] = Y0[m] + s_a (X[m] . A_a^T) . B_a^T        a = the adapter of the segment that row m lies in
 //
-// with A_a [rank][cols], B_a [rows][rank], segments (requests) of any length.  Everything about it is bytes: the adapters
-// are read once, X and Y0 in, Y out, 2 * rank products to a byte or less.  Both products run in one kernel, so T = X . A^T never
+// with A_a [rank][cols], B_a [rows][rank], segments (requests) of any length.  Everything about it is bytes: the adapters in
+// use, X and Y0 in, Y out, 2 * rank products to a byte or less.  Both products run in one kernel, so T = X . A^T never
 // goes to memory.  CTAs of a cluster share the reduction of the first product (a slice of cols each), add up T through
 // distributed shared memory, and share the columns of the second (a slice of rows of B each); T is held in fp32 and enters the
-// second product as two bf16 terms, three where Y is fp32 (2^-18, 2^-27 of it), so that only Y's own rounding shows.
+// second product as two bf16 terms, three where Y is fp32 (which leave out 2^-17, 2^-25 of it), so that only Y's own rounding shows.
 //
 // Segments of up to FEW_ROWS rows (generation) and longer ones (prompts) take different kernels (up to FEW_IN_ALL rows in all, the first), both decide on the
 // device which segments are theirs, and where both are launched they run at the same time:
-//   mwu_adapters_few_kernel   16 rows to a cluster of 8 CTAs, mma.sync straight from global memory (the operands are read once and
-//                             the tensor work is nothing; a lane's eight consecutive elements stand for a permuted reduction order)
+//   mwu_adapters_few_kernel   16 rows of an adapter (of a segment, in batches that are not sorted: an adapter is then read once a
+//                             segment) to a cluster of 2 to 8 CTAs, mma.sync straight from global memory (an item reads its operands
+//                             once and the tensor work is nothing; a lane's eight consecutive elements stand for a permuted reduction order)
 //   mwu_adapters_tile_kernel  128 rows to a cluster of 1 to 8 CTAs, TMA and tcgen05.mma, Y0 and Y through shared memory
 //
 // What bounds them (us a call among others).  Few rows: latency.  One row, rank 16, 4096 -> 4096: 5 on the device (list 1.1, first product 0.7, adding
-// it up 1.7, second 0.8), 8.5 with the host.  64 rows of 32 adapters, rank 32, 4096 -> 16384: 16.9 (3 to sort, 2.5, 3, 5); 73 before loads stood ahead of
+// it up 1.7, second 0.8), 9.5 with the host.  64 rows of 32 adapters, rank 32, 4096 -> 16384: 17.4 (3 to sort, 2.5, 3, 5); 73 before loads stood ahead of
 // tests of their values, 35 before rows were sorted by adapter, 19 with one run of columns at a time; B and Y0 brought to L2 ahead: no
-// faster, and 1 us to ask for.  Many rows: HBM.  8192 rows, rank 64, 4096 -> 4096: 48.5 (X in at 4.1 TB/s, 5 us to add up T, Y0 in and Y out at 5.4).
+// faster, and 1 us to ask for.  Many rows: three phases one after another.  8192 rows, rank 64, 4096 -> 4096: 46.0 (X in at 4.1 TB/s, 5 us to add
+// up T, Y0 in and Y out at 5.4; the tiles that end inside 32 rows, whose boxes leave by plain stores, end last: 49.9 with one store to a lane at a time).
 // Rows without an adapter are copied with eight loads in flight (one: 72 instead of 45 us for that tile).
 //
 // Every wait on an mbarrier is bounded; when one runs out the kernel raises MWU_DEV_TIMEOUT, waits for its copies in
@@ -34,7 +36,7 @@ using namespace gemm;
 
 constexpr int FEW_ROWS = 32;            // rows of a segment that the first kernel takes,
 constexpr int FEW_IN_ALL = 256;         // rows of a call that it takes whatever its segments,
-constexpr int SORTED_ROWS = 512;        // and rows of a call that it sorts by adapter
+constexpr int SORTED_ROWS = 512;        // and rows of a call that it sorts by adapter: as many as sort_rows has place for
 constexpr int FEW_THREADS = 256;
 constexpr int TILE_THREADS = 320;
 constexpr int TILE_ROWS = 128;          // rows of an item of the tile kernel
@@ -130,8 +132,9 @@ static_assert(alignof(Sorter) == 16 && SORTED_ROWS % 4 == 0, "adapters: keys are
 constexpr int NOBODY = 0x7fffffff;
 
 // Returns the number of items, -1 where the list makes no sense.  All threads of the CTA, each placing two rows by counting those that
-// come before them.  (A bitonic sort is a barrier a step: 3.4 us more for 64 rows.  Single tokens, 4 adapters, rank 32, 4096 -> 16384, sorted /
-// segment by segment: 257 rows 25 us / 64, 384 34 / 94, 512 52 / 114.)
+// come before them, which takes the square of the rows: up to all that the arrays hold, sorted is the faster.  (A bitonic sort is a
+// barrier a step: 3.4 us more for 64 rows.  Single tokens, 4 adapters, rank 32, 4096 -> 16384, sorted / segment by segment: 257 rows
+// 25 us / 64, 384 34 / 94, 512 52 / 114.)
 __device__ __forceinline__ int sort_rows(const Params &p, Sorter *o, int per) {
     constexpr int MINE = SORTED_ROWS / FEW_THREADS;
     const int tid = threadIdx.x;
@@ -282,7 +285,7 @@ struct Few {
     __nv_bfloat16 T[TERMS][16][T_LD];
 };
 
-// 16 rows of one segment to a cluster.  First product: CTA c of the cluster takes an eighth of cols in chunks of 32, a warp a
+// 16 rows of one adapter or segment to a cluster.  First product: CTA c of the cluster takes its share of cols in chunks of 32, a warp a
 // chunk at a time: lane (g, t) = (lane / 4, lane % 4) loads elements 8t .. 8t + 7 of the chunk of rows g and g + 8 of X and of rows
 // 8i + g of A, 16 bytes each, and the two MMAs of a chunk take words 0, 1 and 2, 3 of both: the order of the reduction is
 // permuted alike in both operands.  Second product: 32 columns of Y at a time, MMA i multiplying with rows

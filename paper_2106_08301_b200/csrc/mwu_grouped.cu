@@ -21,10 +21,12 @@
 // fp32 results: the tensor core drops what lies below an accumulator's last place (about 1e-9 of the result a product, always
 // towards zero), so sums are taken out of tensor memory every 512 products and added in registers; bf16 results hide it.
 //
-// What bounds it (us a pass among others).  Many rows: the power cap and the loads of full tiles.  16 of 4096 x 4096, 16384 rows: 461,
-// 1.19 PFLOP/s (300 to 357 without the loads); input gradient of 8192 rows 266, alone and cool 217 with the tensor pipe at 70 % and the
-// crossbar at 41 %.  Weight gradients: the fp32 output besides (16 of 2048 x 4096: 325, 253 without the stores; a burst of them
-// from all SMs leaves at 5.8 TB/s).  Few rows: reading the weights (64 of 2048 x 4096, 256 rows: 166, 5.9 TB/s).  Small calls: 2.5 us until the
+// What bounds it (us a pass among others, 3 % either way from one device to the next).  Many rows: loads, and tiles dealt to the pairs
+// in a fixed order.  16 of 4096 x 4096, 16384 rows: 465, 1.18 PFLOP/s (300 to 357 without the loads); input gradient of 8192 rows 268, alone
+// and cool 217 with the tensor pipe at 70 % and the crossbar at 41 %.  At 0.37 us for 256 x 256 x 64 products the busiest pair has 364 of
+// the product's time where the mean is 331, 186 and 170 of the input gradient's, 184 and 169 of the weight gradient's; MN-major operands come
+// in boxes of half a width; one lane issues the MMAs of all tiles; and passes in a row run into the power cap (1.55 GHz).  Weight
+// gradients: the fp32 output besides (16 of 2048 x 4096: 327, 253 without the stores; a burst of them from all SMs leaves at 5.8 TB/s).  Few rows: reading the weights (64 of 2048 x 4096, 256 rows: 166, 5.9 TB/s).  Small calls: 2.5 us until the
 // roles begin, 2.3 until the first stage is there, 2 to 3 from the last MMA to the last store, and 0.27 us a stage whatever is in it.
 // Tried and taken back: weights or activations brought to L2 ahead of their loads (4 to 17 % slower: the copy engine's requests are what
 // is short); tiles of a pair worked out in a table before the first load, and the epilogue's code in one loop (a small call 1.3 us
