@@ -116,7 +116,7 @@ __device__ __forceinline__ bool mbar_test(unsigned bar, unsigned parity) {
     return ok != 0;
 }
 // bounded wait: false when aborted or out of time (then *abort is set)
-__device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatile int *abort, long long limit = WAIT_LIMIT_CYCLES) {
+__device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatile int *abort) {
     // A short wait is polled (a waiter suspended in try_wait wakes a few hundred cycles late); a long
     // one, an epilogue warp waiting out a tile of a long reduction, sleeps in try_wait and leaves the
     // issue slots and the power to the warps that work.
@@ -128,22 +128,22 @@ __device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatil
     while (true) {
         if (mbar_try_wait(bar, parity)) return true;
         if (*abort) return false;
-        if (clock64() - t0 > limit) { *abort = 1; return false; }
+        if (clock64() - t0 > WAIT_LIMIT_CYCLES) { *abort = 1; return false; }
     }
 }
 // the same for a single latency-critical warp (producer, MMA issuer): polled for much longer first
-__device__ __forceinline__ bool mbar_wait_spin(unsigned bar, unsigned parity, volatile int *abort, long long limit = WAIT_LIMIT_CYCLES) {
+__device__ __forceinline__ bool mbar_wait_spin(unsigned bar, unsigned parity, volatile int *abort) {
 #pragma unroll 1
     for (int i = 0; i < 4096; ++i)
         if (mbar_test(bar, parity)) return true;
-    return mbar_wait(bar, parity, abort, limit);
+    return mbar_wait(bar, parity, abort);
 }
 // a whole warp waits, polling for long; the same answer in all lanes
-__device__ __forceinline__ bool warp_wait_spin(unsigned bar, unsigned parity, volatile int *abort, long long limit = WAIT_LIMIT_CYCLES) {
+__device__ __forceinline__ bool warp_wait_spin(unsigned bar, unsigned parity, volatile int *abort) {
 #pragma unroll 1
     for (int i = 0; i < 4096; ++i)
         if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit));
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
 // barrier over the THREADS threads (whole warps) that name barrier `id`
 template <int THREADS>

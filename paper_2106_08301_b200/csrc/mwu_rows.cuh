@@ -14,6 +14,35 @@ struct WaitLimits {
 };
 WaitLimits wait_limits();               // mwu_grouped.cu
 
+// The bounded waits with a limit of the caller's: polled for a while, then asleep in try_wait; false when aborted or out of time (then
+// *abort is set).
+__device__ __forceinline__ bool mbar_wait(unsigned bar, unsigned parity, volatile int *abort, long long limit) {
+#pragma unroll 1
+    for (int i = 0; i < 128; ++i)
+        if (mbar_test(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort) return false;
+        if (clock64() - t0 > limit) { *abort = 1; return false; }
+    }
+}
+// the same for a single latency-critical warp, polled for much longer first: every lane for itself
+__device__ __forceinline__ bool mbar_wait_spin(unsigned bar, unsigned parity, volatile int *abort, long long limit) {
+#pragma unroll 1
+    for (int i = 0; i < 4096; ++i)
+        if (mbar_test(bar, parity)) return true;
+    return mbar_wait(bar, parity, abort, limit);
+}
+// ... and with the same answer in all lanes
+__device__ __forceinline__ bool warp_wait_spin(unsigned bar, unsigned parity, volatile int *abort, long long limit) {
+#pragma unroll 1
+    for (int i = 0; i < 4096; ++i)
+        if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit));
+}
+
 // the two halves of a cluster barrier, for what can be done between them
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
