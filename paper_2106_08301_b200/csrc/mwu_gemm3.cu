@@ -250,6 +250,7 @@ mwu_dense_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
         // hand-over also carries the ring position, so nobody counts the other one's stages.
         const unsigned mine = (warp == 1) ? 0u : 1u;
         bool ok = true, issued_any = false;
+        const bool leader = elect_one();                    // the lane that issues
         const unsigned idesc = make_idesc_pair(256);
         volatile unsigned *ho_tiles = &sm->ho_tiles, *ho_ring = &sm->ho_ring;
         for (long long k = 0; ok && tile_of(k, mt_, nt_); ++k) {
@@ -276,9 +277,9 @@ mwu_dense_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             unsigned phase = ring / D_STAGES;
             tc_fence_after();
             bool first = true;
-            // The stage loop holds no vote and no warp barrier: every lane executes the same barrier
-            // probes as one warp instruction and so takes the same decisions; what the warp does
-            // between two stages has to fit into the time the MMAs of one stage take.
+            // The stage loop holds no vote, no election and no warp barrier: what the warp does between
+            // two stages has to fit into the time the MMAs of one stage take, and where the limit of
+            // a wait runs out lanes may leave the loop at different stages.
             for (int ks = 0; ks < n_stages; ++ks) {
                 const unsigned live = lv[ks];
                 if (!live) continue;
@@ -286,7 +287,7 @@ mwu_dense_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 tc_fence_after();
                 const unsigned long long adesc = make_desc(smem_u32(sA + stage * D_A_BYTES));
                 const unsigned long long bdesc = make_desc(smem_u32(sB + stage * D_B_BYTES));
-                if (elect_one()) {
+                if (leader) {
 #pragma unroll
                     for (int k4 = 0; k4 < 4; ++k4) {
                         if ((live >> k4) & 1u) {
@@ -307,7 +308,7 @@ mwu_dense_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
                 __threadfence_block();
                 *ho_tiles = (unsigned)(k + 1);
             }
-            if (elect_one()) {
+            if (leader) {
                 if (!first) {
                     umma2_commit_both(smem_u32(&sm->tfull[buf]));
                 } else {
@@ -318,7 +319,7 @@ mwu_dense_pair_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_c
             __syncwarp();
         }
         // everything this thread issued must have retired before tensor memory is freed
-        if (lane == 0 && issued_any) {
+        if (leader && issued_any) {
             umma2_commit_local(smem_u32(&sm->drain[mine]));
             mbar_wait(smem_u32(&sm->drain[mine]), 0, abort);
         }
